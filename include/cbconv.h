@@ -372,6 +372,124 @@ int cb_select_thresholds(const cb_stage *stages, int32_t n_stages, const void *c
                          const double *max_loss, void *workspace_dev, size_t workspace_bytes, float *taus_out,
                          double *loss_out, int32_t *steps_out);
 
+/* ---- tokens of a stream: rotary positions, a paged cache, its attention and its eviction ---------------
+ *
+ * What a program keeps of a stream to answer from it: a key and a value per token (of a changed pixel of a feature map,
+ * say), in a cache of fixed-size pages that one new token per sequence reads and that is cut back to a budget.  These calls
+ * keep nothing themselves: every one is described by its arguments, enqueued on hip_stream, asynchronous, and free
+ * of allocations, memsets and host decisions that depend on device data, so it may be captured into a HIP graph.
+ * Values are float32 or bfloat16; everything between them is computed in float32.  Calls that share a cache or a scratch
+ * buffer run on one stream, or are ordered by the caller. */
+
+/* A tensor of heads: value i of head h of token n is data_dev[n * token_stride + h * head_stride + i] (strides in values;
+ * any sign and order, the values of a head are contiguous).  heads * head_dim values a token. */
+typedef struct {
+    const void *data_dev;
+    int64_t token_stride, head_stride;
+    int32_t heads;
+    int32_t reserved;      /* must be zero */
+} cb_heads;
+
+/* Rotary positions with several axes (time, row and column of a token, say).  A head's first 2*n values are n pairs,
+ * n = the sum of pairs[]; the first pairs[0] of them turn with a token's position on axis 0, the next pairs[1] with
+ * that on axis 1, and so on: by position * base^(-i / m) radians, where i counts the pairs from zero over all axes and m = n
+ * (CB_LADDER_SHARED), or starts again with each axis and m = pairs[axis] (CB_LADDER_PER_AXIS).  A pair (x, y) becomes
+ * (x cos - y sin, x sin + y cos).  Values behind the pairs are copied.  Angles are reduced to one turn in float64: they are
+ * exact to float32 at positions up to 2^20, and to 2e-6 radians at any. */
+typedef enum { CB_PAIRS_HALVES = 0, /* pair i: values i and n + i */ CB_PAIRS_ADJACENT = 1 /* 2*i and 2*i + 1 */ } cb_pairs;
+typedef enum { CB_LADDER_SHARED = 0, CB_LADDER_PER_AXIS = 1 } cb_ladder;
+#define CB_ROTARY_MAX_AXES 4
+#define CB_ROTARY_MAX_PAIRS 128
+typedef struct {
+    int32_t head_dim;                      /* a multiple of 8 up to 256 */
+    int32_t n_axes;                        /* 1 .. CB_ROTARY_MAX_AXES */
+    int32_t pairs[CB_ROTARY_MAX_AXES];     /* not negative, zero behind n_axes; 1 <= n <= head_dim / 2 */
+    int32_t layout;                        /* cb_pairs */
+    int32_t ladder;                        /* cb_ladder */
+    float base;                            /* > 0, finite */
+    int32_t reserved;                      /* must be zero */
+} cb_rotary_desc;
+/* The description with its frequencies (turns per unit of position), filled on the host once by cb_rotary_init. */
+typedef struct {
+    cb_rotary_desc desc;
+    double turns[CB_ROTARY_MAX_PAIRS];
+} cb_rotary;
+int cb_rotary_init(const cb_rotary_desc *desc, cb_rotary *rotary);
+
+/* Rotate q, and k with it if not NULL, of n_tokens tokens into q_out and k_out (the same number of heads; an output may be
+ * its own input, with its strides, and overlaps no other tensor).  positions_dev: n_tokens x n_axes.  inverse = 1 turns back:
+ * that is also the gradient with respect to q and k, given the gradients of q_out and k_out.  n_tokens below 2^31, may be 0. */
+int cb_rotate(const cb_rotary *rotary, int32_t dtype, int64_t n_tokens, const int32_t *positions_dev,
+              const cb_heads *q, const cb_heads *q_out, const cb_heads *k, const cb_heads *k_out, int32_t inverse,
+              void *hip_stream);
+
+/* A paged cache of n_seq sequences.  Slot j of sequence s lies in row j % page_tokens of page table_dev[s * max_pages + j /
+ * page_tokens]; a page holds n_kv_heads x page_tokens x head_dim values.  Slots 0 .. lengths_dev[s] - 1 hold tokens, capacity =
+ * max_pages * page_tokens is the most.  All arrays belong to the caller, who fills the table (entries behind a sequence's
+ * last page are not read) and may change it between calls; a page that is written to belongs to one sequence.  What the
+ * host cannot check is checked on the device: lengths are taken as 0 .. capacity, and slots whose page number is
+ * not 0 .. n_pages - 1 hold no token: no page is written or read for them. */
+typedef struct {
+    int32_t n_seq, n_kv_heads;        /* n_seq 1 .. 65535, n_kv_heads 1 .. 1024 */
+    int32_t head_dim;                 /* a multiple of 8 up to 256 */
+    int32_t page_tokens;              /* a power of two, 16 .. 1024 */
+    int32_t max_pages, n_pages;       /* capacity up to 2^30 */
+    int32_t dtype;                    /* cb_dtype */
+    int32_t reserved;                 /* must be zero */
+    void *k_pages_dev, *v_pages_dev;  /* n_pages x n_kv_heads x page_tokens x head_dim each, 16-byte aligned */
+    const int32_t *table_dev;         /* n_seq x max_pages */
+    int32_t *lengths_dev;             /* n_seq */
+    float *weight_dev;                /* n_seq x n_kv_heads x capacity: attention that a slot's token has had, or NULL */
+    int32_t *time_dev;                /* n_seq x n_kv_heads x capacity: a token's position on axis 0, or NULL */
+    void *scratch_dev;                /* cb_cache_scratch_bytes, 256-byte aligned, cleared to zero by the caller once; shared
+                                         by caches whose calls run on one stream.  Calls leave its counters at zero */
+    size_t scratch_bytes;
+} cb_cache;
+/* Scratch for all calls on the cache with up to n_q_heads query heads (0: appending and eviction alone). */
+int cb_cache_scratch_bytes(const cb_cache *cache, int32_t n_q_heads, size_t *bytes);
+
+/* Append tokens: rows offsets_dev[s] .. offsets_dev[s + 1] - 1 of k and v (n_seq + 1 ascending row numbers from 0 on; NULL: row s
+ * alone, n_tokens = n_seq) become slots start_dev[s], start_dev[s] + 1, ... of sequence s (start_dev NULL: lengths_dev, that
+ * is, behind the tokens that are there); lengths_dev[s] becomes start + count, capacity at most: rows beyond it are not
+ * kept.  rotary not NULL: keys are rotated on the way, and q into q_out if q is not NULL (whose row n
+ * belongs to row n of k).  positions_dev: n_tokens x n_axes (n_tokens x 1 without rotary; NULL there: a token's time is its
+ * slot).  weight becomes 0, time the position on axis 0.  Rows from offsets_dev[n_seq] on are ignored, q's too, so
+ * that n_tokens may be an upper bound of a count that only the device knows. */
+int cb_cache_append(const cb_cache *cache, const cb_rotary *rotary, int32_t n_tokens, const int32_t *positions_dev,
+                    const int32_t *offsets_dev, const int32_t *start_dev, const cb_heads *k, const cb_heads *v,
+                    const cb_heads *q, const cb_heads *q_out, void *hip_stream);
+
+/* Attention of one new token per sequence (row s of q and out: sequence s) over the slots of its sequence:
+ *   s_j = scale * q . k_j, capped: softcap * tanh(s_j / softcap) where softcap > 0;  out = sum_j e^(s_j) v_j / sum_j e^(s_j).
+ * q->heads is a multiple of n_kv_heads; query head i reads key head i / (q->heads / n_kv_heads).  lse_dev (may be NULL): n_seq x
+ * q->heads float32, ln of the sum.  A sequence without a token, or with scores of minus infinity alone, gives zeros and minus
+ * infinity.  accumulate = 1 (weight_dev not NULL): weight becomes decay * weight + the sum over the query heads that read it of
+ * e^(s_j - lse), for every slot that holds a token.  The sums' order depends on lengths and sizes alone. */
+typedef struct {
+    float scale, softcap;      /* finite; softcap >= 0, 0: none */
+    float decay;               /* 0 .. 1 */
+    int32_t accumulate;
+    int32_t reserved;          /* must be zero */
+} cb_attend_params;
+int cb_cache_attend(const cb_cache *cache, const cb_attend_params *params, const cb_heads *q, const cb_heads *out,
+                    float *lse_dev, void *hip_stream);
+
+/* Cut every sequence with more than `budget` tokens back to that many, each key head by itself.  Tokens whose time is above the
+ * head's newest - window are kept (the newest `budget` where there are more), and of the others those that have had the most
+ * attention; ties go to the lowest slot, a weight that is not a number counts as the lowest.  Kept tokens from slot `budget` on
+ * move, in ascending order, into the slots below it that became free, in ascending order; a slot whose token stays is not
+ * touched.  (Order does not matter to attention: keys carry their positions.)  weight and time move with their tokens,
+ * lengths become at most `budget`.  weight_in_dev, time_in_dev, lengths_in_dev: what to go by, NULL: the cache's own; if
+ * given, the cache's arrays receive them as they are after the eviction.  The cache needs weight_dev and time_dev. */
+typedef struct {
+    int32_t budget;            /* 1 .. capacity */
+    int32_t window;            /* >= 0 */
+    const float *weight_in_dev;
+    const int32_t *time_in_dev;
+    const int32_t *lengths_in_dev;
+} cb_evict_params;
+int cb_cache_evict(const cb_cache *cache, const cb_evict_params *params, void *hip_stream);
+
 const char *cb_strerror(int status);
 int cb_last_hip_error(void);
 /* Library version: major*10000 + minor*100 + patch. */

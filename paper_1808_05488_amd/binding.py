@@ -32,8 +32,12 @@ EXPORTS = (
     "cb_pool_destroy", "cb_strerror", "cb_last_hip_error", "cb_version",
     "cb_network_forward", "cb_sum_squared_diff", "cb_sum_squared_diff_noalloc", "cb_select_workspace_bytes",
     "cb_select_thresholds",
+    "cb_rotary_init", "cb_rotate", "cb_cache_scratch_bytes", "cb_cache_append", "cb_cache_attend", "cb_cache_evict",
 )
 CB_METRIC_WORKSPACE_BYTES = 4096
+CB_PAIRS_HALVES, CB_PAIRS_ADJACENT = 0, 1
+CB_LADDER_SHARED, CB_LADDER_PER_AXIS = 0, 1
+CB_ROTARY_MAX_AXES, CB_ROTARY_MAX_PAIRS = 4, 128
 
 
 class cb_layer_desc(C.Structure):
@@ -48,6 +52,37 @@ class cb_stage(C.Structure):
 
 class cb_select_params(C.Structure):
     _fields_ = [("tau0", C.c_float), ("factor", C.c_float), ("max_steps", C.c_int32), ("reserved", C.c_int32)]
+
+
+class cb_heads(C.Structure):
+    _fields_ = [("data_dev", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("heads", C.c_int32), ("reserved", C.c_int32)]
+
+
+class cb_rotary_desc(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("n_axes", C.c_int32), ("pairs", C.c_int32 * CB_ROTARY_MAX_AXES),
+                ("layout", C.c_int32), ("ladder", C.c_int32), ("base", C.c_float), ("reserved", C.c_int32)]
+
+
+class cb_rotary(C.Structure):
+    _fields_ = [("desc", cb_rotary_desc), ("turns", C.c_double * CB_ROTARY_MAX_PAIRS)]
+
+
+class cb_cache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seq", "n_kv_heads", "head_dim", "page_tokens", "max_pages", "n_pages",
+                                         "dtype", "reserved")] + \
+               [(n, C.c_void_p) for n in ("k_pages_dev", "v_pages_dev", "table_dev", "lengths_dev", "weight_dev", "time_dev",
+                                          "scratch_dev")] + [("scratch_bytes", C.c_size_t)]
+
+
+class cb_attend_params(C.Structure):
+    _fields_ = [("scale", C.c_float), ("softcap", C.c_float), ("decay", C.c_float), ("accumulate", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class cb_evict_params(C.Structure):
+    _fields_ = [("budget", C.c_int32), ("window", C.c_int32), ("weight_in_dev", C.c_void_p),
+                ("time_in_dev", C.c_void_p), ("lengths_in_dev", C.c_void_p)]
 
 
 class cb_stats(C.Structure):
@@ -113,6 +148,13 @@ def lib():
         L.cb_pool_changes.argtypes = [vp, P(vp)]
         L.cb_pool_out_shape.argtypes = [vp, P(i32), P(i32), P(i32)]
         L.cb_pool_destroy.argtypes = [vp]
+        L.cb_rotary_init.argtypes = [P(cb_rotary_desc), P(cb_rotary)]
+        L.cb_rotate.argtypes = [P(cb_rotary), i32, C.c_int64, vp, P(cb_heads), P(cb_heads), P(cb_heads), P(cb_heads), i32, vp]
+        L.cb_cache_scratch_bytes.argtypes = [P(cb_cache), i32, P(sz)]
+        L.cb_cache_append.argtypes = [P(cb_cache), P(cb_rotary), i32, vp, vp, vp, P(cb_heads), P(cb_heads), P(cb_heads),
+                                      P(cb_heads), vp]
+        L.cb_cache_attend.argtypes = [P(cb_cache), P(cb_attend_params), P(cb_heads), P(cb_heads), vp, vp]
+        L.cb_cache_evict.argtypes = [P(cb_cache), P(cb_evict_params), vp]
         L.cb_strerror.argtypes = [C.c_int]
         L.cb_strerror.restype = C.c_char_p
         L.cb_last_hip_error.restype = C.c_int
@@ -555,3 +597,178 @@ class Pool:
 
     def changes(self) -> torch.Tensor:
         return _view(self.state_buf, cb_pool_changes(self.handle), (self.Hp, self.Wp), torch.uint8)
+
+
+# ---------------------------------------------------------------- tokens of a stream
+_CB_DT = {torch.float32: CB_F32, torch.bfloat16: CB_BF16}
+
+
+def _stream(device) -> Optional[int]:
+    return torch.cuda.current_stream(device).cuda_stream or None
+
+
+def _heads(t: torch.Tensor, what: str, like: torch.Tensor, dim: int, heads: Optional[int] = None,
+           tokens: Optional[int] = None) -> cb_heads:
+    """A tokens x heads x head_dim tensor whose heads are contiguous, as the ABI takes it."""
+    shape = t.shape
+    assert t.dtype == like.dtype and t.device == like.device, f"{what}: {t.dtype} on {t.device}, not {like.dtype} on {like.device}"
+    assert len(shape) == 3 and shape[2] == dim and (t.stride(2) == 1 or t.numel() == 0), f"{what}: shape {tuple(shape)}, strides {t.stride()}"
+    assert heads is None or shape[1] == heads, f"{what}: {shape[1]} heads, not {heads}"
+    assert tokens is None or shape[0] == tokens, f"{what}: {shape[0]} tokens, not {tokens}"
+    return cb_heads(t.data_ptr(), t.stride(0), t.stride(1), shape[1], 0)
+
+
+def _ints(t: Optional[torch.Tensor], what: str, device, *shape) -> Optional[int]:
+    """Address of a dense int32 array of that shape (None: not given)."""
+    if t is None:
+        return None
+    assert t.dtype == torch.int32 and t.device == device and t.is_contiguous() and tuple(t.shape) == shape, \
+        f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, not a dense int32 {shape} on {device}"
+    return t.data_ptr()
+
+
+class Rotary:
+    """Rotary positions with several axes: pairs[a] pairs of a head turn with a token's position on axis a."""
+
+    def __init__(self, head_dim: int, pairs, base: float = 10000.0, layout: int = CB_PAIRS_HALVES, ladder: int = CB_LADDER_SHARED):
+        pairs = [int(n) for n in pairs]
+        assert len(pairs) <= CB_ROTARY_MAX_AXES
+        d = cb_rotary_desc()
+        d.head_dim, d.n_axes, d.layout, d.ladder, d.base = head_dim, len(pairs), layout, ladder, base
+        for a, n in enumerate(pairs):
+            d.pairs[a] = n
+        self.head_dim, self.n_axes = head_dim, len(pairs)
+        self.plan = cb_rotary()
+        _check(lib().cb_rotary_init(C.byref(d), C.byref(self.plan)), "cb_rotary_init")
+        self._ref = C.byref(self.plan)
+
+    def rotate(self, q: torch.Tensor, positions: torch.Tensor, k: Optional[torch.Tensor] = None, inverse: bool = False,
+               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+        """q (tokens x heads x head_dim) turned by positions (tokens x axes, int32), and k with it: q_out, or (q_out, k_out).
+        inverse: turned back, which is also the gradient of q from that of q_out.  An output may be its input."""
+        n = q.shape[0]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        a, b = _heads(q, "q", q, self.head_dim), _heads(q_out, "q_out", q, self.head_dim, q.shape[1], n)
+        c = d = None
+        if k is not None:
+            if k_out is None:
+                k_out = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+            c = C.byref(_heads(k, "k", q, self.head_dim, None, n))
+            d = C.byref(_heads(k_out, "k_out", q, self.head_dim, k.shape[1], n))
+        _check(lib().cb_rotate(self._ref, _CB_DT[q.dtype], n, _ints(positions, "positions", q.device, n, self.n_axes),
+                               C.byref(a), C.byref(b), c, d, int(inverse), _stream(q.device)), "cb_rotate")
+        return q_out if k is None else (q_out, k_out)
+
+
+class TokenCache:
+    """A paged key-value cache (cb_cache) over tensors of the caller's, and its scratch buffer.
+
+    k_pages, v_pages: pages x key heads x page_tokens x head_dim; table: sequences x pages of a sequence, int32; lengths:
+    sequences, int32; weight (float32) and time (int32): sequences x key heads x capacity, needed to evict.  Calls run on
+    the current stream; calls that share a cache or a scratch buffer have to be on one stream, or ordered."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+                 weight: Optional[torch.Tensor] = None, time: Optional[torch.Tensor] = None,
+                 scratch: Optional[torch.Tensor] = None):
+        assert k_pages.is_cuda and k_pages.dim() == 4 and k_pages.is_contiguous() and k_pages.dtype in _CB_DT
+        assert v_pages.device == k_pages.device and v_pages.dtype == k_pages.dtype and v_pages.is_contiguous()
+        assert v_pages.shape == k_pages.shape and table.dim() == 2
+        n_pages, heads, page, dim = k_pages.shape
+        self.n_seq, self.n_kv_heads, self.head_dim, self.capacity = table.shape[0], heads, dim, table.shape[1] * page
+        self.device = k_pages.device
+        self.desc = d = cb_cache()
+        d.n_seq, d.n_kv_heads, d.head_dim, d.page_tokens = self.n_seq, heads, dim, page
+        d.max_pages, d.n_pages, d.dtype = table.shape[1], n_pages, _CB_DT[k_pages.dtype]
+        d.k_pages_dev, d.v_pages_dev = k_pages.data_ptr(), v_pages.data_ptr()
+        d.table_dev = _ints(table, "table", self.device, self.n_seq, table.shape[1])
+        d.lengths_dev = _ints(lengths, "lengths", self.device, self.n_seq)
+        if weight is not None:
+            d.weight_dev = self._floats(weight)
+        d.time_dev = _ints(time, "time", self.device, self.n_seq, heads, self.capacity)
+        self.k_pages, self.v_pages, self.table, self.lengths, self.weight, self.time = k_pages, v_pages, table, lengths, weight, time
+        self._ref = C.byref(d)
+        self._room = -1                    # query heads that the scratch buffer has room for
+        self._scratch(0, scratch)
+
+    @classmethod
+    def create(cls, n_seq: int, n_kv_heads: int, head_dim: int, capacity: int, dtype=torch.bfloat16, page_tokens: int = 64,
+               device="cuda", evictable: bool = True):
+        """An empty cache whose pages belong to the sequences in order."""
+        pages = -(-capacity // page_tokens)
+        shape = (n_seq * pages, n_kv_heads, page_tokens, head_dim)
+        table = torch.arange(n_seq * pages, dtype=torch.int32, device=device).view(n_seq, pages)
+        slots = (n_seq, n_kv_heads, pages * page_tokens)
+        return cls(torch.zeros(shape, dtype=dtype, device=device), torch.zeros(shape, dtype=dtype, device=device), table,
+                   torch.zeros(n_seq, dtype=torch.int32, device=device),
+                   torch.zeros(slots, dtype=torch.float32, device=device) if evictable else None,
+                   torch.zeros(slots, dtype=torch.int32, device=device) if evictable else None)
+
+    def _floats(self, t: torch.Tensor) -> int:
+        assert t.dtype == torch.float32 and t.device == self.device and t.is_contiguous()
+        assert tuple(t.shape) == (self.n_seq, self.n_kv_heads, self.capacity), tuple(t.shape)
+        return t.data_ptr()
+
+    def scratch_bytes(self, n_q_heads: int) -> int:
+        n = C.c_size_t()
+        _check(lib().cb_cache_scratch_bytes(self._ref, n_q_heads, C.byref(n)), "cb_cache_scratch_bytes")
+        return n.value
+
+    def _scratch(self, n_q_heads: int, given: Optional[torch.Tensor] = None):
+        if n_q_heads <= self._room:
+            return
+        nbytes = self.scratch_bytes(n_q_heads)
+        if given is None and self._room >= 0 and self.scratch.numel() >= nbytes:
+            given = self.scratch
+        if given is None:
+            given = _alloc(nbytes, self.device)
+            given.zero_()
+        self.scratch, self._room = given, n_q_heads
+        self.desc.scratch_dev, self.desc.scratch_bytes = given.data_ptr(), given.numel() * given.element_size()
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
+               q: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None, start: Optional[torch.Tensor] = None,
+               q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """Rows offsets[s] .. offsets[s + 1] - 1 of k and v (without offsets row s) behind the tokens of sequence s, or from
+        slot start[s] on; keys rotated if there is a rotary, and q (row for row), which is returned."""
+        n, like = k.shape[0], self.k_pages
+        a = _heads(k, "k", like, self.head_dim, self.n_kv_heads)
+        b = _heads(v, "v", like, self.head_dim, self.n_kv_heads, n)
+        c = d = None
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            c = C.byref(_heads(q, "q", like, self.head_dim, None, n))
+            d = C.byref(_heads(q_out, "q_out", like, self.head_dim, q.shape[1], n))
+        _check(lib().cb_cache_append(self._ref, rotary._ref if rotary is not None else None, n,
+                                     _ints(positions, "positions", self.device, n, rotary.n_axes if rotary is not None else 1),
+                                     _ints(offsets, "offsets", self.device, self.n_seq + 1), _ints(start, "start", self.device, self.n_seq),
+                                     C.byref(a), C.byref(b), c, d, _stream(self.device)), "cb_cache_append")
+        return q_out
+
+    def attend(self, q: torch.Tensor, scale: Optional[float] = None, softcap: float = 0.0, accumulate: bool = False,
+               decay: float = 1.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+        """(out, lse) of one query token per sequence (q: sequences x query heads x head_dim).  scale: 1 / sqrt(head_dim) if not
+        given.  accumulate: the cache's weight becomes decay * weight + the weights of this call."""
+        heads = q.shape[1]
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty((self.n_seq, heads), dtype=torch.float32, device=q.device)
+        assert lse.dtype == torch.float32 and lse.device == self.device and lse.is_contiguous() and tuple(lse.shape) == (self.n_seq, heads)
+        a = _heads(q, "q", self.k_pages, self.head_dim, None, self.n_seq)
+        b = _heads(out, "out", self.k_pages, self.head_dim, heads, self.n_seq)
+        self._scratch(heads)
+        p = cb_attend_params(self.head_dim ** -0.5 if scale is None else scale, softcap, decay, int(accumulate), 0)
+        _check(lib().cb_cache_attend(self._ref, C.byref(p), C.byref(a), C.byref(b), lse.data_ptr(), _stream(self.device)),
+               "cb_cache_attend")
+        return out, lse
+
+    def evict(self, budget: int, window: int = 0, weight: Optional[torch.Tensor] = None, time: Optional[torch.Tensor] = None,
+              lengths: Optional[torch.Tensor] = None) -> None:
+        """Cut every sequence back to `budget` tokens a key head: those of the newest `window` steps of time, then those with the
+        most weight.  weight, time, lengths: what to go by instead of the cache's own, which receive what is left."""
+        p = cb_evict_params(budget, window, None if weight is None else self._floats(weight),
+                            _ints(time, "time", self.device, self.n_seq, self.n_kv_heads, self.capacity),
+                            _ints(lengths, "lengths", self.device, self.n_seq))
+        _check(lib().cb_cache_evict(self._ref, C.byref(p), _stream(self.device)), "cb_cache_evict")

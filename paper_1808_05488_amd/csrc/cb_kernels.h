@@ -8,6 +8,9 @@
 
 namespace cb {
 
+// Keeps the code for cb_last_hip_error() and returns CB_EHIP.
+int note_hip_error(hipError_t e);
+
 // Optional pair of events that receive the begin and end time stamps of one
 // kernel dispatch (per-step timing); null events make this a plain launch.
 struct Tm {

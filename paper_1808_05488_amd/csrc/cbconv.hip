@@ -28,6 +28,12 @@ std::atomic<int> g_scan_wait_limit{kScanWaitDefault};
 constexpr int kPatience = 4096;
 
 inline int hip_fail(hipError_t e) { g_last_hip = (int)e; return CB_EHIP; }
+}  // namespace
+
+int cb::note_hip_error(hipError_t e) { return hip_fail(e); }
+
+namespace {
+
 #define CB_HIP(expr) do { hipError_t e_ = (expr); if (e_ != hipSuccess) return hip_fail(e_); } while (0)
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
