@@ -440,7 +440,7 @@ typedef struct {
     const int32_t *table_dev;         /* n_seq x max_pages */
     int32_t *lengths_dev;             /* n_seq */
     float *weight_dev;                /* n_seq x n_kv_heads x capacity: attention that a slot's token has had, or NULL */
-    int32_t *time_dev;                /* n_seq x n_kv_heads x capacity: a token's position on axis 0, or NULL */
+    int32_t *time_dev;                /* n_seq x n_kv_heads x capacity: a token's position on axis 0, or NULL; both 16-byte aligned */
     void *scratch_dev;                /* cb_cache_scratch_bytes, 256-byte aligned, cleared to zero by the caller once; shared
                                          by caches whose calls run on one stream.  Calls leave its counters at zero */
     size_t scratch_bytes;
@@ -463,7 +463,7 @@ int cb_cache_append(const cb_cache *cache, const cb_rotary *rotary, int32_t n_to
  *   s_j = scale * q . k_j, capped: softcap * tanh(s_j / softcap) where softcap > 0;  out = sum_j e^(s_j) v_j / sum_j e^(s_j).
  * q->heads is a multiple of n_kv_heads; query head i reads key head i / (q->heads / n_kv_heads).  lse_dev (may be NULL): n_seq x
  * q->heads float32, ln of the sum.  A sequence without a token, or with scores of minus infinity alone, gives zeros and minus
- * infinity.  accumulate = 1 (weight_dev not NULL): weight becomes decay * weight + the sum over the query heads that read it of
+ * infinity.  n_seq * capacity * (key heads times blocks of 16 of their query heads) stays below 2^39.  accumulate = 1 (weight_dev not NULL): weight becomes decay * weight + the sum over the query heads that read it of
  * e^(s_j - lse), for every slot that holds a token.  The sums' order depends on lengths and sizes alone. */
 typedef struct {
     float scale, softcap;      /* finite; softcap >= 0, 0: none */

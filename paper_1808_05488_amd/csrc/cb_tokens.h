@@ -63,6 +63,7 @@ struct AttendJob {
     float scale, softcap, decay;
     int accumulate;
 };
+bool attend_fits(const Cache& c, int q_heads);      // its work can be counted in 32 bits
 hipError_t launch_attend(const AttendJob& j, const Cache& c, hipStream_t st);
 
 struct EvictJob {

@@ -61,6 +61,7 @@ int check_cache(const cb_cache* d, bool scratch, int q_heads, Cache* c)
     c->scratch = static_cast<char*>(d->scratch_dev);
     if (!scratch) return CB_OK;
     if (!c->k || !c->v || ((uintptr_t)c->k & 15) || ((uintptr_t)c->v & 15) || !c->table || !c->lengths) return CB_EINVAL;
+    if (((uintptr_t)c->weight & 15) || ((uintptr_t)c->time & 15)) return CB_EINVAL;
     if (!c->scratch || ((uintptr_t)c->scratch & 255)) return CB_EINVAL;
     if (d->scratch_bytes < scratch_plan(*c, q_heads).total) return CB_ENOMEM;
     return CB_OK;
@@ -212,6 +213,7 @@ int cb_cache_attend(const cb_cache* cache, const cb_attend_params* params, const
     if (q->heads != out->heads || q->heads % c.heads) return CB_EINVAL;
     if (params->accumulate && !c.weight) return CB_EINVAL;
     CB_CHECKED(cb::check_cache(cache, true, q->heads, &c));
+    if (!cb::attend_fits(c, q->heads)) return CB_EINVAL;
     j.lse = lse_dev;
     j.scale = params->scale; j.softcap = params->softcap; j.decay = params->decay;
     j.accumulate = params->accumulate;
