@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -148,13 +149,13 @@ def lib():
         L.cb_pool_changes.argtypes = [vp, P(vp)]
         L.cb_pool_out_shape.argtypes = [vp, P(i32), P(i32), P(i32)]
         L.cb_pool_destroy.argtypes = [vp]
-        L.cb_rotary_init.argtypes = [P(cb_rotary_desc), P(cb_rotary)]
-        L.cb_rotate.argtypes = [P(cb_rotary), i32, C.c_int64, vp, P(cb_heads), P(cb_heads), P(cb_heads), P(cb_heads), i32, vp]
-        L.cb_cache_scratch_bytes.argtypes = [P(cb_cache), i32, P(sz)]
-        L.cb_cache_append.argtypes = [P(cb_cache), P(cb_rotary), i32, vp, vp, vp, P(cb_heads), P(cb_heads), P(cb_heads),
-                                      P(cb_heads), vp]
-        L.cb_cache_attend.argtypes = [P(cb_cache), P(cb_attend_params), P(cb_heads), P(cb_heads), vp, vp]
-        L.cb_cache_evict.argtypes = [P(cb_cache), P(cb_evict_params), vp]
+        # (structures by address: byref(), bytes or the address itself)
+        L.cb_rotary_init.argtypes = [vp, vp]
+        L.cb_rotate.argtypes = [vp, i32, C.c_int64, vp, vp, vp, vp, vp, i32, vp]
+        L.cb_cache_scratch_bytes.argtypes = [vp, i32, P(sz)]
+        L.cb_cache_append.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.cb_cache_attend.argtypes = [vp, vp, vp, vp, vp, vp]
+        L.cb_cache_evict.argtypes = [vp, vp, vp]
         L.cb_strerror.argtypes = [C.c_int]
         L.cb_strerror.restype = C.c_char_p
         L.cb_last_hip_error.restype = C.c_int
@@ -601,29 +602,34 @@ class Pool:
 
 # ---------------------------------------------------------------- tokens of a stream
 _CB_DT = {torch.float32: CB_F32, torch.bfloat16: CB_BF16}
+# The structures of one call, packed anew for it (a call may run while another thread packs its own).  A call's work on the host is
+# part of a small call's time: packing takes 0.2 us a structure, filling a ctypes one 0.5 us.
+_pack_heads = struct.Struct("@Pqqii").pack
+_pack_attend = struct.Struct("@fffii").pack
+_pack_evict = struct.Struct("@iiPPP").pack
+assert struct.calcsize("@Pqqii") == C.sizeof(cb_heads) and struct.calcsize("@fffii") == C.sizeof(cb_attend_params)
+assert struct.calcsize("@iiPPP") == C.sizeof(cb_evict_params)
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _stream(device) -> Optional[int]:
-    return torch.cuda.current_stream(device).cuda_stream or None
+def _heads(t: torch.Tensor, what: str, dtype, index: int, dim: int, heads: Optional[int] = None, tokens: Optional[int] = None) -> bytes:
+    """A tokens x heads x head_dim tensor whose heads are contiguous, as the ABI takes it (cb_heads)."""
+    shape, stride = t.shape, t.stride()
+    if not (t.dtype is dtype and t.get_device() == index and len(shape) == 3 and shape[2] == dim and
+            (stride[2] == 1 or t.numel() == 0) and (heads is None or shape[1] == heads) and (tokens is None or shape[0] == tokens)):
+        raise AssertionError(f"{what}: {t.dtype} {tuple(shape)}, strides {stride}, on {t.device}; needed: {dtype} "
+                             f"({'tokens' if tokens is None else tokens}, {'heads' if heads is None else heads}, {dim}), "
+                             f"contiguous heads, on GPU {index}")
+    return _pack_heads(t.data_ptr(), stride[0], stride[1], shape[1], 0)
 
 
-def _heads(t: torch.Tensor, what: str, like: torch.Tensor, dim: int, heads: Optional[int] = None,
-           tokens: Optional[int] = None) -> cb_heads:
-    """A tokens x heads x head_dim tensor whose heads are contiguous, as the ABI takes it."""
-    shape = t.shape
-    assert t.dtype == like.dtype and t.device == like.device, f"{what}: {t.dtype} on {t.device}, not {like.dtype} on {like.device}"
-    assert len(shape) == 3 and shape[2] == dim and (t.stride(2) == 1 or t.numel() == 0), f"{what}: shape {tuple(shape)}, strides {t.stride()}"
-    assert heads is None or shape[1] == heads, f"{what}: {shape[1]} heads, not {heads}"
-    assert tokens is None or shape[0] == tokens, f"{what}: {shape[0]} tokens, not {tokens}"
-    return cb_heads(t.data_ptr(), t.stride(0), t.stride(1), shape[1], 0)
-
-
-def _ints(t: Optional[torch.Tensor], what: str, device, *shape) -> Optional[int]:
-    """Address of a dense int32 array of that shape (None: not given)."""
+def _dense(t: Optional[torch.Tensor], what: str, dtype, index: int, shape) -> Optional[int]:
+    """Address of a dense array of that type and shape (None: not given)."""
     if t is None:
         return None
-    assert t.dtype == torch.int32 and t.device == device and t.is_contiguous() and tuple(t.shape) == shape, \
-        f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, not a dense int32 {shape} on {device}"
+    if not (t.dtype is dtype and t.get_device() == index and t.shape == shape and t.is_contiguous()):
+        raise AssertionError(f"{what}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}; needed: dense {dtype} {tuple(shape)} on GPU {index}")
     return t.data_ptr()
 
 
@@ -640,24 +646,26 @@ class Rotary:
         self.head_dim, self.n_axes = head_dim, len(pairs)
         self.plan = cb_rotary()
         _check(lib().cb_rotary_init(C.byref(d), C.byref(self.plan)), "cb_rotary_init")
-        self._ref = C.byref(self.plan)
+        self._address = C.addressof(self.plan)
 
     def rotate(self, q: torch.Tensor, positions: torch.Tensor, k: Optional[torch.Tensor] = None, inverse: bool = False,
                q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
         """q (tokens x heads x head_dim) turned by positions (tokens x axes, int32), and k with it: q_out, or (q_out, k_out).
         inverse: turned back, which is also the gradient of q from that of q_out.  An output may be its input."""
-        n = q.shape[0]
+        n, dtype, index, dim = q.shape[0], q.dtype, q.get_device(), self.head_dim
+        assert index >= 0 and dtype in _CB_DT, f"q: {dtype} on {q.device}"
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        a, b = _heads(q, "q", q, self.head_dim), _heads(q_out, "q_out", q, self.head_dim, q.shape[1], n)
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        a, b = _heads(q, "q", dtype, index, dim), _heads(q_out, "q_out", dtype, index, dim, q.shape[1], n)
         c = d = None
         if k is not None:
             if k_out is None:
-                k_out = torch.empty(k.shape, dtype=q.dtype, device=q.device)
-            c = C.byref(_heads(k, "k", q, self.head_dim, None, n))
-            d = C.byref(_heads(k_out, "k_out", q, self.head_dim, k.shape[1], n))
-        _check(lib().cb_rotate(self._ref, _CB_DT[q.dtype], n, _ints(positions, "positions", q.device, n, self.n_axes),
-                               C.byref(a), C.byref(b), c, d, int(inverse), _stream(q.device)), "cb_rotate")
+                k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+            c, d = _heads(k, "k", dtype, index, dim, None, n), _heads(k_out, "k_out", dtype, index, dim, k.shape[1], n)
+        status = lib().cb_rotate(self._address, _CB_DT[dtype], n, _dense(positions, "positions", torch.int32, index, (n, self.n_axes)),
+                                 a, b, c, d, 1 if inverse else 0, _raw_stream(index))
+        if status:
+            _check(status, "cb_rotate")
         return q_out if k is None else (q_out, k_out)
 
 
@@ -671,24 +679,25 @@ class TokenCache:
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
                  weight: Optional[torch.Tensor] = None, time: Optional[torch.Tensor] = None,
                  scratch: Optional[torch.Tensor] = None):
-        assert k_pages.is_cuda and k_pages.dim() == 4 and k_pages.is_contiguous() and k_pages.dtype in _CB_DT
-        assert v_pages.device == k_pages.device and v_pages.dtype == k_pages.dtype and v_pages.is_contiguous()
-        assert v_pages.shape == k_pages.shape and table.dim() == 2
+        assert k_pages.is_cuda and k_pages.dim() == 4 and k_pages.dtype in _CB_DT and table.dim() == 2
         n_pages, heads, page, dim = k_pages.shape
         self.n_seq, self.n_kv_heads, self.head_dim, self.capacity = table.shape[0], heads, dim, table.shape[1] * page
-        self.device = k_pages.device
+        self.device, self.dtype, self._index = k_pages.device, k_pages.dtype, k_pages.get_device()
+        self._slots = (self.n_seq, heads, self.capacity)
+        i = self._index
         self.desc = d = cb_cache()
         d.n_seq, d.n_kv_heads, d.head_dim, d.page_tokens = self.n_seq, heads, dim, page
-        d.max_pages, d.n_pages, d.dtype = table.shape[1], n_pages, _CB_DT[k_pages.dtype]
-        d.k_pages_dev, d.v_pages_dev = k_pages.data_ptr(), v_pages.data_ptr()
-        d.table_dev = _ints(table, "table", self.device, self.n_seq, table.shape[1])
-        d.lengths_dev = _ints(lengths, "lengths", self.device, self.n_seq)
-        if weight is not None:
-            d.weight_dev = self._floats(weight)
-        d.time_dev = _ints(time, "time", self.device, self.n_seq, heads, self.capacity)
+        d.max_pages, d.n_pages, d.dtype = table.shape[1], n_pages, _CB_DT[self.dtype]
+        d.k_pages_dev = _dense(k_pages, "k_pages", self.dtype, i, k_pages.shape)
+        d.v_pages_dev = _dense(v_pages, "v_pages", self.dtype, i, k_pages.shape)
+        d.table_dev = _dense(table, "table", torch.int32, i, table.shape)
+        d.lengths_dev = _dense(lengths, "lengths", torch.int32, i, (self.n_seq,))
+        d.weight_dev = _dense(weight, "weight", torch.float32, i, self._slots)
+        d.time_dev = _dense(time, "time", torch.int32, i, self._slots)
         self.k_pages, self.v_pages, self.table, self.lengths, self.weight, self.time = k_pages, v_pages, table, lengths, weight, time
-        self._ref = C.byref(d)
+        self._address = C.addressof(d)
         self._room = -1                    # query heads that the scratch buffer has room for
+        self._lse = {}                     # by query heads: what an lse is like
         self._scratch(0, scratch)
 
     @classmethod
@@ -704,71 +713,75 @@ class TokenCache:
                    torch.zeros(slots, dtype=torch.float32, device=device) if evictable else None,
                    torch.zeros(slots, dtype=torch.int32, device=device) if evictable else None)
 
-    def _floats(self, t: torch.Tensor) -> int:
-        assert t.dtype == torch.float32 and t.device == self.device and t.is_contiguous()
-        assert tuple(t.shape) == (self.n_seq, self.n_kv_heads, self.capacity), tuple(t.shape)
-        return t.data_ptr()
-
     def scratch_bytes(self, n_q_heads: int) -> int:
         n = C.c_size_t()
-        _check(lib().cb_cache_scratch_bytes(self._ref, n_q_heads, C.byref(n)), "cb_cache_scratch_bytes")
+        _check(lib().cb_cache_scratch_bytes(self._address, n_q_heads, C.byref(n)), "cb_cache_scratch_bytes")
         return n.value
 
     def _scratch(self, n_q_heads: int, given: Optional[torch.Tensor] = None):
-        if n_q_heads <= self._room:
-            return
         nbytes = self.scratch_bytes(n_q_heads)
         if given is None and self._room >= 0 and self.scratch.numel() >= nbytes:
             given = self.scratch
         if given is None:
             given = _alloc(nbytes, self.device)
             given.zero_()
+        assert given.dtype == torch.uint8 and given.device == self.device and given.is_contiguous()
         self.scratch, self._room = given, n_q_heads
-        self.desc.scratch_dev, self.desc.scratch_bytes = given.data_ptr(), given.numel() * given.element_size()
+        self.desc.scratch_dev, self.desc.scratch_bytes = given.data_ptr(), given.numel()
 
     def append(self, k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
                q: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None, start: Optional[torch.Tensor] = None,
                q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """Rows offsets[s] .. offsets[s + 1] - 1 of k and v (without offsets row s) behind the tokens of sequence s, or from
         slot start[s] on; keys rotated if there is a rotary, and q (row for row), which is returned."""
-        n, like = k.shape[0], self.k_pages
-        a = _heads(k, "k", like, self.head_dim, self.n_kv_heads)
-        b = _heads(v, "v", like, self.head_dim, self.n_kv_heads, n)
+        n, dtype, i, dim = k.shape[0], self.dtype, self._index, self.head_dim
+        a = _heads(k, "k", dtype, i, dim, self.n_kv_heads)
+        b = _heads(v, "v", dtype, i, dim, self.n_kv_heads, n)
         c = d = None
         if q is not None:
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            c = C.byref(_heads(q, "q", like, self.head_dim, None, n))
-            d = C.byref(_heads(q_out, "q_out", like, self.head_dim, q.shape[1], n))
-        _check(lib().cb_cache_append(self._ref, rotary._ref if rotary is not None else None, n,
-                                     _ints(positions, "positions", self.device, n, rotary.n_axes if rotary is not None else 1),
-                                     _ints(offsets, "offsets", self.device, self.n_seq + 1), _ints(start, "start", self.device, self.n_seq),
-                                     C.byref(a), C.byref(b), c, d, _stream(self.device)), "cb_cache_append")
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            c, d = _heads(q, "q", dtype, i, dim, None, n), _heads(q_out, "q_out", dtype, i, dim, q.shape[1], n)
+        status = lib().cb_cache_append(
+            self._address, None if rotary is None else rotary._address, n,
+            _dense(positions, "positions", torch.int32, i, (n, 1 if rotary is None else rotary.n_axes)),
+            _dense(offsets, "offsets", torch.int32, i, (self.n_seq + 1,)), _dense(start, "start", torch.int32, i, (self.n_seq,)),
+            a, b, c, d, _raw_stream(i))
+        if status:
+            _check(status, "cb_cache_append")
         return q_out
 
     def attend(self, q: torch.Tensor, scale: Optional[float] = None, softcap: float = 0.0, accumulate: bool = False,
                decay: float = 1.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
         """(out, lse) of one query token per sequence (q: sequences x query heads x head_dim).  scale: 1 / sqrt(head_dim) if not
         given.  accumulate: the cache's weight becomes decay * weight + the weights of this call."""
+        dtype, i, dim = self.dtype, self._index, self.head_dim
+        a = _heads(q, "q", dtype, i, dim, None, self.n_seq)
         heads = q.shape[1]
+        if heads > self._room:
+            self._scratch(heads)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         if lse is None:
-            lse = torch.empty((self.n_seq, heads), dtype=torch.float32, device=q.device)
-        assert lse.dtype == torch.float32 and lse.device == self.device and lse.is_contiguous() and tuple(lse.shape) == (self.n_seq, heads)
-        a = _heads(q, "q", self.k_pages, self.head_dim, None, self.n_seq)
-        b = _heads(out, "out", self.k_pages, self.head_dim, heads, self.n_seq)
-        self._scratch(heads)
-        p = cb_attend_params(self.head_dim ** -0.5 if scale is None else scale, softcap, decay, int(accumulate), 0)
-        _check(lib().cb_cache_attend(self._ref, C.byref(p), C.byref(a), C.byref(b), lse.data_ptr(), _stream(self.device)),
-               "cb_cache_attend")
+            like = self._lse.get(heads)
+            if like is None:
+                like = self._lse[heads] = torch.empty((self.n_seq, heads), dtype=torch.float32, device=self.device)
+            lse = torch.empty_like(like)
+        b = _heads(out, "out", dtype, i, dim, heads, self.n_seq)
+        status = lib().cb_cache_attend(self._address, _pack_attend(dim ** -0.5 if scale is None else scale, softcap, decay, 1 if accumulate else 0, 0),
+                                       a, b, _dense(lse, "lse", torch.float32, i, (self.n_seq, heads)), _raw_stream(i))
+        if status:
+            _check(status, "cb_cache_attend")
         return out, lse
 
     def evict(self, budget: int, window: int = 0, weight: Optional[torch.Tensor] = None, time: Optional[torch.Tensor] = None,
               lengths: Optional[torch.Tensor] = None) -> None:
         """Cut every sequence back to `budget` tokens a key head: those of the newest `window` steps of time, then those with the
         most weight.  weight, time, lengths: what to go by instead of the cache's own, which receive what is left."""
-        p = cb_evict_params(budget, window, None if weight is None else self._floats(weight),
-                            _ints(time, "time", self.device, self.n_seq, self.n_kv_heads, self.capacity),
-                            _ints(lengths, "lengths", self.device, self.n_seq))
-        _check(lib().cb_cache_evict(self._ref, C.byref(p), _stream(self.device)), "cb_cache_evict")
+        i = self._index
+        status = lib().cb_cache_evict(self._address, _pack_evict(
+            budget, window, _dense(weight, "weight", torch.float32, i, self._slots) or 0,
+            _dense(time, "time", torch.int32, i, self._slots) or 0, _dense(lengths, "lengths", torch.int32, i, (self.n_seq,)) or 0),
+            _raw_stream(i))
+        if status:
+            _check(status, "cb_cache_evict")
