@@ -479,8 +479,8 @@ int cb_cache_attend(const cb_cache *cache, const cb_attend_params *params, const
  * attention; ties go to the lowest slot, a weight that is not a number counts as the lowest.  Kept tokens from slot `budget` on
  * move, in ascending order, into the slots below it that became free, in ascending order; a slot whose token stays is not
  * touched.  (Order does not matter to attention: keys carry their positions.)  weight and time move with their tokens,
- * lengths become at most `budget`.  weight_in_dev, time_in_dev, lengths_in_dev: what to go by, NULL: the cache's own; if
- * given, the cache's arrays receive them as they are after the eviction.  The cache needs weight_dev and time_dev. */
+ * lengths become at most `budget`.  weight_in_dev, time_in_dev, lengths_in_dev: what to go by (the first two 16-byte
+ * aligned), NULL: the cache's own; if given, the cache's arrays receive them as they are after the eviction.  The cache needs weight_dev and time_dev. */
 typedef struct {
     int32_t budget;            /* 1 .. capacity */
     int32_t window;            /* >= 0 */

@@ -1,26 +1,40 @@
 // Eviction from a paged cache by accumulated attention weight.
 //
 // Every (sequence, key head) keeps `budget` of its tokens: the recent ones (time above the newest - window), then those with the
-// largest weight.  One workgroup each finds the smallest kept rank by counting the ranks' bytes from the highest to the lowest (radix
+// largest weight.  One workgroup each finds the smallest kept rank by counting the ranks' digits from the highest to the lowest (radix
 // selection: no sorting), and lists, in ascending order, the free slots below the budget and the kept tokens above it.
 // There are as many of one as of the other; a second launch moves them.  Sources and targets never overlap, so nothing waits
 // for anything, and only what has to move moves.
+//
+// The selection reads weights and times from memory at once, and keeps the ranks in LDS, where the counting's passes find
+// them; those of more slots than it holds are made again from memory in every pass.
 #include "cb_tokens.h"
 
 namespace cb {
 
 namespace {
 
-constexpr int THREADS = 1024, WAVES = THREADS / 64, COPIES = 32;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int THREADS = 1024, WAVES = THREADS / 64;
+constexpr int DIGIT = 10, BINS = 1 << DIGIT;      // bits of a digit; a bin a thread
+constexpr int COPIES = 4;                        // of a histogram: lanes that count the same digit do not queue up behind each other
+constexpr int STRIDE = 4 * THREADS, ROUNDS = 8;  // four slots a thread a round
+constexpr int LDS_RANKS = 31744;
+static_assert(BINS == THREADS && LDS_RANKS <= STRIDE * ROUNDS && 2 * 64 == ROUNDS * WAVES, "a bin a thread, two counts a lane");
 
 struct EvictArgs {
     EvictJob j;
     Cache c;
     int32_t *count, *hole, *mover;       // per (sequence, head): how many, their slots (pitch = capacity)
     int copies;                          // weight or time have to be copied where a token stays
+    int room;                            // ranks that LDS holds: up to 4 * ROUNDS a thread
 };
 
-// In the order of the numbers; what is not a number comes first, and zeros are equal.
+// In the order of the numbers; what is not a number comes first, and zeros are equal.  Rank 0 is for what is below all others: weights that
+// are not a number, the earliest time there is, and the slots up to three behind the last token, which come behind all tokens of rank 0.
 __device__ __forceinline__ uint32_t ordered(float f)
 {
     if (f != f) return 0u;
@@ -28,164 +42,318 @@ __device__ __forceinline__ uint32_t ordered(float f)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ uint32_t ordered(int32_t t) { return (uint32_t)t ^ 0x80000000u; }
+constexpr uint32_t RECENT = 0xFFFFFFFFu;         // above every weight's rank
 
-// What decides about a slot.
-struct Ranks {
-    const float* weight;
-    const int32_t* time;
-    long newest;          // - window: times above it are recent
-    bool by_time;         // there are as many recent tokens as the budget holds: the newest of them
-    __device__ bool recent(int i) const { return (long)time[i] > newest; }
-    // rank among the tokens that compete; in: does it compete
-    __device__ uint32_t rank(int i, bool* in) const
+// The sum over the lanes before this one, and over all.
+__device__ __forceinline__ int lane_sum_before(int v, int* all)
+{
+    const int sum = wave_scan(v);
+    *all = __builtin_amdgcn_readlane(sum, 63);
+    return (int)((uint32_t)sum - (uint32_t)v);
+}
+
+// Counts of rounds and wavefronts, in that order: what comes before a wavefront's share of each round, and all.
+struct Shares {
+    int one, below;       // of rounds' entries 2 * lane; sum before it
+    int all;
+    __device__ Shares(const int* s_count, int entries)
     {
-        if (by_time) { *in = true; return ordered(time[i]); }
-        *in = !recent(i);
-        return ordered(weight[i]);
+        const int lane = threadIdx.x & 63;
+        one = 2 * lane < entries ? s_count[2 * lane] : 0;
+        below = lane_sum_before((int)((uint32_t)one + (2 * lane < entries ? (uint32_t)s_count[2 * lane + 1] : 0u)), &all);
+    }
+    __device__ int before(int entry) const
+    {
+        return (int)((uint32_t)__builtin_amdgcn_readlane(below, entry >> 1) + (entry & 1 ? (uint32_t)__builtin_amdgcn_readlane(one, entry >> 1) : 0u));
     }
 };
 
-__device__ int block_sum(int v, int* s_part)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    int sum = 0;
-    for (int w = 0; w < WAVES; ++w) sum += s_part[w];
-    return sum;
-}
-
+// ALL_IN_LDS: of every sequence that the cache has room for.  Its 1024 threads take 8.5 us for 8 heads of 2 358 tokens (512: 9.1, 256: 10.3), mostly
+// the latency of about 20 steps that follow from each other, and 25 us for 128 heads of 17 000 - 25 000.
+template <bool ALL_IN_LDS>
 __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
 {
-    __shared__ int hist[256 * COPIES];
-    __shared__ int s_bin[256];
-    __shared__ int s_part[WAVES], s_hole[WAVES], s_mover[WAVES];
-    __shared__ int s_pick, s_left;
+    extern __shared__ __align__(16) uint32_t s_rank[];
+    __shared__ __align__(16) int hist[BINS * COPIES];
+    __shared__ int s_part[WAVES], s_equal[ROUNDS * WAVES], s_moves[ROUNDS * WAVES];
+    __shared__ int s_newest, s_recent, s_pick[3];
+    __shared__ uint32_t s_low, s_high;
     const Cache& c = a.c;
-    const int seq = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int seq = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const long pair = (long)seq * c.heads + h, at = pair * c.capacity;
     const int len = clamp_length(a.j.lengths_in[seq], c.capacity), budget = a.j.budget;
-    Ranks r{a.j.weight_in + at, a.j.time_in + at, 0, false};
+    const float* weight = a.j.weight_in + at;
+    const int32_t* time = a.j.time_in + at;
 
+    if (tid == 0) {
+        s_newest = INT32_MIN;
+        s_recent = 0;
+        s_low = 0xFFFFFFFFu;
+        s_high = 0;
+    }
+    // Times and weights, four slots a thread (a row ends behind a multiple of 16).  Where others than the cache's own decide, the cache
+    // receives them: of free slots too, which the moves write over.
+    const bool in_lds = ALL_IN_LDS || len <= a.room;
+    int newest = INT32_MIN;
+    i32x4 t[ROUNDS];
+    // (both as read: then as the ranks want them)
+    auto take_over = [&](int i, i32x4& t, f32x4& w) {
+        if (a.copies && i < budget) {
+            if (i + 4 <= budget && i + 4 <= len) {
+                *reinterpret_cast<f32x4*>(c.weight + at + i) = w;
+                *reinterpret_cast<i32x4*>(c.time + at + i) = t;
+            } else
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    if (i + x < budget && i + x < len) {
+                        c.weight[at + i + x] = w[x];
+                        c.time[at + i + x] = t[x];
+                    }
+        }
+        if (i + 4 > len)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                if (i + x >= len) {
+                    t[x] = INT32_MIN;
+                    w[x] = __builtin_nanf("");
+                }
+    };
+    if (in_lds) {
+        // (all loads at once; times stay where they are)
+        f32x4 w[ROUNDS];
+#pragma unroll
+        for (int n = 0; n < ROUNDS; ++n)
+            if (n * STRIDE + 4 * tid < len) {
+                t[n] = *reinterpret_cast<const i32x4*>(time + n * STRIDE + 4 * tid);
+                w[n] = *reinterpret_cast<const f32x4*>(weight + n * STRIDE + 4 * tid);
+            }
+#pragma unroll
+        for (int n = 0; n < ROUNDS; ++n) {
+            const int i = n * STRIDE + 4 * tid;
+            if (i < len) {
+                take_over(i, t[n], w[n]);
+                *reinterpret_cast<u32x4*>(s_rank + i) = u32x4{ordered(w[n][0]), ordered(w[n][1]), ordered(w[n][2]), ordered(w[n][3])};
+                newest = max(max(newest, max(t[n][0], t[n][1])), max(t[n][2], t[n][3]));
+            }
+        }
+    } else {
+        for (int i = 4 * tid; i < len; i += STRIDE) {
+            i32x4 u = *reinterpret_cast<const i32x4*>(time + i);
+            f32x4 w = *reinterpret_cast<const f32x4*>(weight + i);
+            take_over(i, u, w);
+            newest = max(max(newest, max(u[0], u[1])), max(u[2], u[3]));
+        }
+    }
     if (len <= budget) {
         if (tid == 0) a.count[pair] = 0;
-        if (a.copies)
-            for (int i = tid; i < len; i += THREADS) {
-                c.weight[at + i] = r.weight[i];
-                c.time[at + i] = r.time[i];
-            }
         return;
     }
-
-    int newest = INT32_MIN;
-    for (int i = tid; i < len; i += THREADS) newest = max(newest, r.time[i]);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) newest = max(newest, __shfl_xor(newest, d));
-    if (lane == 0) s_part[wave] = newest;
+    newest = wave_max(newest);
     __syncthreads();
-    for (int w = 0; w < WAVES; ++w) newest = max(newest, s_part[w]);
-    r.newest = (long)newest - a.j.window;
-    int recent = 0;
-    for (int i = tid; i < len; i += THREADS) recent += r.recent(i);
-    recent = block_sum(recent, s_part);
-    r.by_time = recent >= budget;
+    if (lane == 0) atomicMax(&s_newest, newest);
+    __syncthreads();
+    // times from here on are recent, if any are
+    const long from = (long)s_newest - a.j.window + 1;
+    const int recent_from = from < INT32_MIN ? INT32_MIN : (from > INT32_MAX ? INT32_MAX : (int)from);
+    const bool any_recent = a.j.window > 0;
+    bool by_time = false;
+    auto ranks_of = [&](const i32x4& t, const u32x4& of_weight) {
+        u32x4 k;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) k[x] = by_time ? ordered(t[x]) : (any_recent && t[x] >= recent_from ? RECENT : of_weight[x]);
+        return k;
+    };
+    auto ranks = [&](int i) -> u32x4 {                         // of slots i .. i + 3
+        if (in_lds) return *reinterpret_cast<const u32x4*>(s_rank + i);
+        const f32x4 w = *reinterpret_cast<const f32x4*>(weight + i);
+        u32x4 k = ranks_of(*reinterpret_cast<const i32x4*>(time + i), u32x4{ordered(w[0]), ordered(w[1]), ordered(w[2]), ordered(w[3])});
+#pragma unroll
+        for (int x = 1; x < 4; ++x) k[x] = i + x < len ? k[x] : 0u;
+        return k;
+    };
 
-    // the rank of the last token that is kept (`least`), and how many of that rank are
-    int left = r.by_time ? budget : budget - recent;
-    uint32_t least = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        __syncthreads();
-        for (int i = tid; i < 256 * COPIES; i += THREADS) hist[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < len; i += THREADS) {
-            bool in;
-            const uint32_t k = r.rank(i, &in);
-            if (in && (shift == 24 || (k ^ least) >> (shift + 8) == 0))
-                atomicAdd(&hist[((k >> shift) & 255) * COPIES + (lane & (COPIES - 1))], 1);
-        }
-        __syncthreads();
-        if (tid < 256) {
-            int sum = 0;
-            for (int x = 0; x < COPIES; ++x) sum += hist[tid * COPIES + ((x + tid) & (COPIES - 1))];
-            s_bin[tid] = sum;
-        }
-        __syncthreads();
-        if (wave == 0) {
-            // from the highest byte down: lane takes four
-            int n[4], sum = 0;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) sum += n[x] = s_bin[255 - 4 * lane - x];
-            int above = sum;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const int up = __shfl_up(above, d);
-                if (lane >= d) above += up;
-            }
-            above -= sum;
+    // All that rank above `least` stay, and the first `left` of those that rank at it.
+    int left;
+#pragma unroll 1
+    for (;;) {
+        // how many are recent, and between which ranks the others are (rank 0 left aside)
+        int recent = 0, all;
+        uint32_t low = 0xFFFFFFFFu, high = 0;
+        auto note = [&](const u32x4& k) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                if (above < left && above + n[x] >= left) { s_pick = 255 - 4 * lane - x; s_left = left - above; }
-                above += n[x];
+                const bool out = !by_time && k[x] == RECENT;
+                recent += out;
+                low = min(low, k[x] - 1u);
+                high = out ? high : max(high, k[x]);
+            }
+        };
+        if (in_lds) {
+#pragma unroll
+            for (int n = 0; n < ROUNDS; ++n) {
+                const int i = n * STRIDE + 4 * tid;
+                if (i < len) {
+                    const u32x4 k = ranks_of(t[n], *reinterpret_cast<const u32x4*>(s_rank + i));
+                    *reinterpret_cast<u32x4*>(s_rank + i) = k;
+                    note(k);
+                }
+            }
+        } else
+            for (int i = 4 * tid; i < len; i += STRIDE) note(ranks(i));
+        low = ~wave_max_unsigned(~low);
+        high = wave_max_unsigned(high);
+        lane_sum_before(recent, &all);
+        if (lane == 0) {
+            atomicMin(&s_low, low);
+            atomicMax(&s_high, high);
+            atomicAdd(&s_recent, all);
+        }
+        __syncthreads();
+        left = by_time ? budget : budget - s_recent;
+        if (left > 0) break;
+        // there are as many recent tokens as the budget holds: the newest of all are kept
+        by_time = true;
+        __syncthreads();
+        if (tid == 0) { s_low = 0xFFFFFFFFu; s_high = 0; }
+        __syncthreads();
+    }
+    // (there are more others than are left to keep, since there are more tokens than the budget holds)
+    const uint32_t low = s_low + 1u, range = s_high - low;     // (none above rank 0: nothing is in a range that begins behind its end)
+    bool at_zero = s_high == 0;
+    uint32_t least = 0;
+    int shift = 32 - __builtin_clz(range | 1) - DIGIT;
+#pragma unroll 1
+    for (int past = 32; s_high != 0;) {
+        shift = shift < 0 ? 0 : shift;
+        *reinterpret_cast<i32x4*>(hist + 4 * tid) = i32x4{0, 0, 0, 0};
+        __syncthreads();
+        // (recent tokens are out of range but where the range ends with them: then there are none)
+#pragma unroll 2
+        for (int i = 4 * tid; i < len; i += STRIDE) {
+            const u32x4 r = ranks(i);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const uint32_t k = r[x] - low;
+                if (k <= range && (past == 32 || (k ^ least) >> past == 0))
+                    atomicAdd(&hist[((k >> shift) & (BINS - 1)) * COPIES + (lane & (COPIES - 1))], 1);
             }
         }
         __syncthreads();
-        least |= (uint32_t)s_pick << shift;
-        left = s_left;
-    }
-
-    // a wavefront's stretch of slots
-    const int per = (len + THREADS - 1) / THREADS * 64, from = wave * per < len ? wave * per : len, to = from + per < len ? from + per : len;
-    auto state = [&](int i, bool* equal) {                  // kept whatever the others of the last rank do
-        bool in;
-        const uint32_t k = r.rank(i, &in);
-        *equal = in && k == least;
-        return !in || k > least;
-    };
-    int equals = 0;
-    for (int i0 = from; i0 < to; i0 += 64) {
-        bool equal = false;
-        if (i0 + lane < to) state(i0 + lane, &equal);
-        equals += __popcll(__ballot(equal));
-    }
-    __syncthreads();
-    if (lane == 0) s_part[wave] = equals;
-    __syncthreads();
-    int before = 0;
-    for (int w = 0; w < wave; ++w) before += s_part[w];
-    const unsigned long long below = (1ull << lane) - 1;
-    int holes = 0, movers = 0;
-    for (int pass = 0; pass < 2; ++pass) {
-        int run = before;
-        if (pass == 1) {
-            if (lane == 0) { s_hole[wave] = holes; s_mover[wave] = movers; }
-            __syncthreads();
-            holes = movers = 0;
-            for (int w = 0; w < wave; ++w) { holes += s_hole[w]; movers += s_mover[w]; }
+        // from the highest digit down, a digit a thread
+        const int digit = BINS - 1 - tid;
+        const i32x4 bin = *reinterpret_cast<const i32x4*>(hist + digit * COPIES);
+        const int n = bin[0] + bin[1] + bin[2] + bin[3];
+        int all, counted;
+        int above = lane_sum_before(n, &all);
+        if (lane == 0) s_part[wave] = all;
+        __syncthreads();
+        above += __builtin_amdgcn_readlane(lane_sum_before(lane < WAVES ? s_part[lane] : 0, &counted), wave);
+        if (past == 32 && counted < left) {
+            // fewer than are left: all of them stay, and the first of rank 0
+            left -= counted;
+            at_zero = true;
+            break;
         }
-        for (int i0 = from; i0 < to; i0 += 64) {
-            const int i = i0 + lane;
-            bool equal = false, kept = false;
-            if (i < to) kept = state(i, &equal);
-            const unsigned long long eq = __ballot(equal);
-            if (equal) kept = run + __popcll(eq & below) < left;
-            run += __popcll(eq);
-            const bool hole = i < to && !kept && i < budget, mover = kept && i >= budget;
-            const unsigned long long hb = __ballot(hole), mb = __ballot(mover);
-            if (pass == 1) {
-                if (hole) a.hole[at + holes + __popcll(hb & below)] = i;
-                if (mover) a.mover[at + movers + __popcll(mb & below)] = i;
-                if (a.copies && kept && i < budget) {
-                    c.weight[at + i] = r.weight[i];
-                    c.time[at + i] = r.time[i];
+        if (above < left && above + n >= left) {
+            s_pick[0] = digit;
+            s_pick[1] = left - above;
+            s_pick[2] = n;
+        }
+        __syncthreads();
+        least |= (uint32_t)s_pick[0] << shift;
+        left = s_pick[1];
+        if (shift > 0 && left == s_pick[2]) {
+            // all of them stay, whatever their lower digits (there are others below: low + least is not zero)
+            --least;
+            left = 0;
+            break;
+        }
+        if (shift == 0) break;
+        past = shift;
+        shift -= DIGIT;
+    }
+    least = at_zero ? 0u : least + low;
+
+    // Which stay, and where the free slots and the tokens that move into them come in their lists.  Slots come in order of round,
+    // wavefront, lane; as many rounds at a time as counts fit.
+    int equals = 0, holes = 0, movers = 0;                     // so far
+    for (int base = 0; base < len; base += ROUNDS * STRIDE) {
+        const int rounds = (len - base + STRIDE - 1) / STRIDE < ROUNDS ? (len - base + STRIDE - 1) / STRIDE : ROUNDS;
+        uint32_t kept = 0, equal = 0;                          // four bits a round
+        int before[ROUNDS];
+#pragma unroll
+        for (int n = 0; n < ROUNDS; ++n) {
+            const int i = base + n * STRIDE + 4 * tid;
+            if (n < rounds && i < len) {
+                const u32x4 k = ranks(i);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    kept |= (uint32_t)(k[x] > least) << (4 * n + x);
+                    equal |= (uint32_t)(k[x] == least) << (4 * n + x);
                 }
             }
-            holes += __popcll(hb);
-            movers += __popcll(mb);
         }
+        if (left > 0) {
+#pragma unroll
+            for (int n = 0; n < ROUNDS; ++n) {
+                if (n < rounds) {
+                    int all;
+                    before[n] = lane_sum_before((int)__popc(equal >> (4 * n) & 15), &all);
+                    if (lane == 0) s_equal[n * WAVES + wave] = all;
+                }
+            }
+            __syncthreads();
+            const Shares shares(s_equal, rounds * WAVES);
+#pragma unroll
+            for (int n = 0; n < ROUNDS; ++n) {
+                if (n < rounds) {
+                    int at_least = equals + shares.before(n * WAVES + wave) + before[n];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        if (equal >> (4 * n + x) & 1) {
+                            kept |= (uint32_t)(at_least < left) << (4 * n + x);
+                            ++at_least;
+                        }
+                }
+            }
+            equals += shares.all;
+        }
+        // both counts in one number: there are 2^15 slots at most
+        const int last = budget < len ? budget : len;
+#pragma unroll
+        for (int n = 0; n < ROUNDS; ++n) {
+            if (n < rounds) {
+                const int i = base + n * STRIDE + 4 * tid;
+                const uint32_t low4 = i + 4 <= last ? 15u : (i >= last ? 0u : (1u << (last - i)) - 1);
+                const uint32_t k = kept >> (4 * n) & 15;
+                int all;
+                before[n] = lane_sum_before((int)((uint32_t)__popc(low4 & ~k) | (uint32_t)__popc(k & ~low4) << 16), &all);
+                if (lane == 0) s_moves[n * WAVES + wave] = all;
+            }
+        }
+        __syncthreads();
+        const Shares shares(s_moves, rounds * WAVES);
+#pragma unroll
+        for (int n = 0; n < ROUNDS; ++n) {
+            if (n < rounds) {
+                const int i = base + n * STRIDE + 4 * tid;
+                if (s_moves[n * WAVES + wave] != 0) {          // something of this wavefront's moves
+                    const uint32_t both = (uint32_t)before[n] + (uint32_t)shares.before(n * WAVES + wave);
+                    int hole = holes + (int)(both & 0xFFFF), mover = movers + (int)(both >> 16);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const bool stays = kept >> (4 * n + x) & 1;
+                        if (i + x < last && !stays) a.hole[at + hole++] = i + x;
+                        if (i + x >= budget && stays) a.mover[at + mover++] = i + x;
+                    }
+                }
+            }
+        }
+        holes += shares.all & 0xFFFF;
+        movers += (int)((uint32_t)shares.all >> 16);
+        __syncthreads();
     }
-    if (wave == WAVES - 1 && lane == 0) a.count[pair] = movers;
+    if (tid == 0) a.count[pair] = movers;
 }
 
 // Moves: 16-byte pieces of keys and values, weight and time; the sequences' lengths.
@@ -201,21 +369,23 @@ __global__ __launch_bounds__(256) void move_kernel(const EvictArgs a)
         if ((unsigned)page >= (unsigned)c.n_pages) return -1;
         return ((((long)page * c.heads + h) << c.page_shift) + (slot & ((1 << c.page_shift) - 1))) * pieces;
     };
-    uint4 *k = (uint4*)c.k, *v = (uint4*)c.v;
-    for (long i = blockIdx.x * 256 + threadIdx.x; i < (long)n * pieces; i += gridDim.x * 256) {
-        const int m = (int)(i / pieces), p = (int)(i - (long)m * pieces);
-        const int from = a.mover[at + m], to = a.hole[at + m];
-        const long src = row(from), dst = row(to);
-        if (src >= 0 && dst >= 0) {
-            const uint4 x = k[src + p], y = v[src + p];
-            k[dst + p] = x;
-            v[dst + p] = y;
+    u32x4 *k = (u32x4*)c.k, *v = (u32x4*)c.v;
+    // a thread's piece p of its rows
+    const int at_once = 256 / pieces, r = threadIdx.x / pieces, p = threadIdx.x - r * pieces;
+    if (r < at_once)
+        for (int m = blockIdx.x * at_once + r; m < n; m += gridDim.x * at_once) {
+            const int from = a.mover[at + m], to = a.hole[at + m];
+            const long src = row(from), dst = row(to);
+            if (src >= 0 && dst >= 0) {
+                const u32x4 x = __builtin_nontemporal_load(k + src + p), y = __builtin_nontemporal_load(v + src + p);
+                __builtin_nontemporal_store(x, k + dst + p);
+                __builtin_nontemporal_store(y, v + dst + p);
+            }
+            if (p == 0) {
+                c.weight[at + to] = a.j.weight_in[at + from];
+                c.time[at + to] = a.j.time_in[at + from];
+            }
         }
-        if (p == 0) {
-            c.weight[at + to] = a.j.weight_in[at + from];
-            c.time[at + to] = a.j.time_in[at + from];
-        }
-    }
     if (h == 0 && blockIdx.x == 0 && threadIdx.x == 0) {
         const int len = clamp_length(a.j.lengths_in[seq], c.capacity);
         c.lengths[seq] = len < a.j.budget ? len : a.j.budget;
@@ -235,7 +405,10 @@ hipError_t launch_evict(const EvictJob& j, const Cache& c, hipStream_t st)
     a.hole = a.count + pairs;
     a.mover = a.hole + pairs * c.capacity;
     a.copies = j.weight_in != c.weight || j.time_in != c.time;
-    hipLaunchKernelGGL(select_kernel, dim3(c.heads, c.seqs), dim3(THREADS), 0, st, a);
+    a.room = c.capacity < LDS_RANKS ? c.capacity : LDS_RANKS;
+    const dim3 grid(c.heads, c.seqs), block(THREADS);
+    if (c.capacity <= LDS_RANKS) hipLaunchKernelGGL(select_kernel<true>, grid, block, a.room * 4, st, a);
+    else hipLaunchKernelGGL(select_kernel<false>, grid, block, a.room * 4, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     // workgroups of the moves: a few for each compute unit, no more than the most there can be to move

@@ -15,6 +15,23 @@ constexpr int MAX_ANGLES = 256;                  // of a workgroup
 
 template <typename T, int VE> struct alignas(sizeof(T) * VE) Vec { T e[VE]; };
 
+template <int BYTES> struct Word;
+template <> struct Word<16> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
+template <> struct Word<8> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+template <> struct Word<4> { typedef uint32_t type; };
+template <> struct Word<2> { typedef uint16_t type; };
+// Values pass through once: around the caches.
+template <typename V> __device__ __forceinline__ V load_once(const void* p)
+{
+    typedef typename Word<sizeof(V)>::type W;
+    return __builtin_bit_cast(V, __builtin_nontemporal_load(reinterpret_cast<const W*>(p)));
+}
+template <typename V> __device__ __forceinline__ void store_once(const V& v, void* p)
+{
+    typedef typename Word<sizeof(V)>::type W;
+    __builtin_nontemporal_store(__builtin_bit_cast(W, v), reinterpret_cast<W*>(p));
+}
+
 // Where a token goes in the cache.
 struct Place {
     long row;      // value offset of head 0's row in the pages, -1: nowhere
@@ -142,8 +159,8 @@ __global__ __launch_bounds__(THREADS) void rotary_kernel(const RotaryJob j, cons
         int lo = 2 * VE * piece, hi = lo + VE;
         if (turns && !j.adjacent) lo = VE * piece, hi = n + lo;
         const bool two = hi < j.dim;
-        V a = *reinterpret_cast<const V*>(src + lo), b = a;
-        if (two) b = *reinterpret_cast<const V*>(src + hi);
+        V a = load_once<V>(src + lo), b = a;
+        if (two) b = load_once<V>(src + hi);
         if (turns) {
             const float2* at = cs + t * n + piece * VE;
             V u, v;
@@ -166,8 +183,8 @@ __global__ __launch_bounds__(THREADS) void rotary_kernel(const RotaryJob j, cons
             a = u;
             b = v;
         }
-        *reinterpret_cast<V*>(dst + lo) = a;
-        if (two) *reinterpret_cast<V*>(dst + hi) = b;
+        store_once(a, dst + lo);
+        if (two) store_once(b, dst + hi);
     }
     if (PAGED) {
         for (int i = tid; i < here * c.heads; i += THREADS) {

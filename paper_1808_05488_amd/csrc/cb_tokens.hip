@@ -231,6 +231,7 @@ int cb_cache_evict(const cb_cache* cache, const cb_evict_params* params, void* h
     j.budget = params->budget; j.window = params->window;
     j.weight_in = params->weight_in_dev ? params->weight_in_dev : c.weight;
     j.time_in = params->time_in_dev ? params->time_in_dev : c.time;
+    if (((uintptr_t)j.weight_in & 15) || ((uintptr_t)j.time_in & 15)) return CB_EINVAL;
     j.lengths_in = params->lengths_in_dev ? params->lengths_in_dev : c.lengths;
     CB_LAUNCHED(cb::launch_evict(j, c, (hipStream_t)hip_stream));
     return CB_OK;
