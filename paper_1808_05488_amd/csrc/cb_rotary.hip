@@ -10,6 +10,7 @@ namespace cb {
 namespace {
 
 constexpr int THREADS = 256;
+constexpr int BATCH = 3;                         // items of a thread at a time
 constexpr int MAX_TOKENS = 8;                    // of a workgroup
 constexpr int MAX_ANGLES = 256;                  // of a workgroup
 
@@ -20,16 +21,18 @@ template <> struct Word<16> { typedef uint32_t type __attribute__((ext_vector_ty
 template <> struct Word<8> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 template <> struct Word<4> { typedef uint32_t type; };
 template <> struct Word<2> { typedef uint16_t type; };
-// Values pass through once: around the caches.
-template <typename V> __device__ __forceinline__ V load_once(const void* p)
+// Values of a rotation pass through once: around the caches (38 400 x 40 heads of 128: 147 -> 137 us).  Those of an append
+// end in rows of many pages, and are better gathered in the caches on their way (35 000 tokens, 48 heads: 176 us, 204 around them).
+template <bool CACHED, typename V> __device__ __forceinline__ V load_once(const void* p)
 {
     typedef typename Word<sizeof(V)>::type W;
-    return __builtin_bit_cast(V, __builtin_nontemporal_load(reinterpret_cast<const W*>(p)));
+    return CACHED ? *reinterpret_cast<const V*>(p) : __builtin_bit_cast(V, __builtin_nontemporal_load(reinterpret_cast<const W*>(p)));
 }
-template <typename V> __device__ __forceinline__ void store_once(const V& v, void* p)
+template <bool CACHED, typename V> __device__ __forceinline__ void store_once(const V& v, void* p)
 {
     typedef typename Word<sizeof(V)>::type W;
-    __builtin_nontemporal_store(__builtin_bit_cast(W, v), reinterpret_cast<W*>(p));
+    if (CACHED) *reinterpret_cast<V*>(p) = v;
+    else __builtin_nontemporal_store(__builtin_bit_cast(W, v), reinterpret_cast<W*>(p));
 }
 
 // Where a token goes in the cache.
@@ -100,6 +103,39 @@ __global__ __launch_bounds__(THREADS) void rotary_kernel(const RotaryJob j, cons
     const int tid = threadIdx.x, n = j.pairs;
     const long tok0 = (long)blockIdx.x * tt;
     const int here = (int)(j.tokens - tok0 < tt ? j.tokens - tok0 : tt);
+    const int hq = j.q.heads, hk = j.k.heads, heads = hq + hk + (PAGED ? j.v.heads : 0);
+    const unsigned per_token = (unsigned)heads * pieces, total = per_token * here;
+    const int turned = n / VE;
+
+    // BATCH items a thread at a time, the first of them on their way while the angles are made
+    struct Item { unsigned t, h, piece; };
+    auto item = [&](unsigned it) {
+        Item x;
+        x.t = it / per_token;
+        const unsigned r = it - x.t * per_token;
+        x.h = r / pieces;
+        x.piece = r - x.h * pieces;
+        return x;
+    };
+    auto turns = [&](const Item& x) { return (int)x.piece < turned && (int)x.h < hq + hk; };
+    auto first = [&](const Item& x) { return turns(x) && !j.adjacent ? VE * x.piece : 2 * VE * x.piece; };
+    auto second = [&](const Item& x) { return turns(x) && !j.adjacent ? n + VE * x.piece : 2 * VE * x.piece + VE; };
+    V a[BATCH], b[BATCH];
+    auto fetch = [&](unsigned base) {
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const unsigned it = base + u * THREADS;
+            if (it >= total) continue;
+            const Item x = item(it);
+            const bool q = (int)x.h < hq, k = !PAGED || (int)x.h < hq + hk;
+            const Heads& from = q ? j.q : (k ? j.k : j.v);
+            const T* src = (const T*)from.data + (tok0 + x.t) * from.token + (long)((int)x.h - (q ? 0 : (k ? hq : hq + hk))) * from.head;
+            const int hi = second(x);
+            a[u] = load_once<PAGED, V>(src + first(x));
+            if (hi < j.dim) b[u] = load_once<PAGED, V>(src + hi);
+        }
+    };
+    fetch(tid);
 
     if (PAGED && tid >= THREADS - MAX_TOKENS && tid - (THREADS - MAX_TOKENS) < here)
         find_place(j, c, tok0 + tid - (THREADS - MAX_TOKENS), &place[tid - (THREADS - MAX_TOKENS)]);
@@ -131,60 +167,51 @@ __global__ __launch_bounds__(THREADS) void rotary_kernel(const RotaryJob j, cons
         }
     }
 
-    const int hq = j.q.heads, hk = j.k.heads, heads = hq + hk + (PAGED ? j.v.heads : 0);
-    const unsigned per_token = (unsigned)heads * pieces, total = per_token * here;
-    const int turned = n / VE;
-    for (unsigned it = tid; it < total; it += THREADS) {
-        const unsigned t = it / per_token, r = it - t * per_token, h = r / pieces, piece = r - h * pieces;
-        const long tok = tok0 + t;
-        const T* src;
-        T* dst;
-        bool turns = (int)piece < turned;
-        if ((int)h < hq) {
-            src = (const T*)j.q.data + tok * j.q.token + (long)h * j.q.head;
-            dst = (T*)j.q_out.data + tok * j.q_out.token + (long)h * j.q_out.head;
-            if (PAGED && place[t].ignored) continue;
-        } else if (!PAGED) {
-            src = (const T*)j.k.data + tok * j.k.token + (long)(h - hq) * j.k.head;
-            dst = (T*)j.k_out.data + tok * j.k_out.token + (long)(h - hq) * j.k_out.head;
-        } else {
-            const bool key = (int)h < hq + hk;
-            const int g = key ? h - hq : h - hq - hk;
-            const Heads& from = key ? j.k : j.v;
-            if (place[t].row < 0) continue;
-            src = (const T*)from.data + tok * from.token + (long)g * from.head;
-            dst = (T*)(key ? c.k : c.v) + place[t].row + (((long)g * c.dim) << c.page_shift);
-            turns = turns && key;
-        }
-        int lo = 2 * VE * piece, hi = lo + VE;
-        if (turns && !j.adjacent) lo = VE * piece, hi = n + lo;
-        const bool two = hi < j.dim;
-        V a = load_once<V>(src + lo), b = a;
-        if (two) b = load_once<V>(src + hi);
-        if (turns) {
-            const float2* at = cs + t * n + piece * VE;
-            V u, v;
+    for (unsigned base = tid; base < total;) {
 #pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                if (!j.adjacent || VE == 1) {
-                    const float x = widen(a.e[e]), y = widen(b.e[e]);
-                    narrow(x * at[e].x - y * at[e].y, u.e[e]);
-                    narrow(x * at[e].y + y * at[e].x, v.e[e]);
-                } else if ((e & 1) == 0) {
-                    const int f = VE > 1 ? e + 1 : e;      // (there is one: VE is even here)
-                    const float2 s = at[e / 2], w = at[VE / 2 + e / 2];
-                    const float x = widen(a.e[e]), y = widen(a.e[f]), z = widen(b.e[e]), q = widen(b.e[f]);
-                    narrow(x * s.x - y * s.y, u.e[e]);
-                    narrow(x * s.y + y * s.x, u.e[f]);
-                    narrow(z * w.x - q * w.y, v.e[e]);
-                    narrow(z * w.y + q * w.x, v.e[f]);
-                }
+        for (int u = 0; u < BATCH; ++u) {
+            const unsigned it = base + u * THREADS;
+            if (it >= total) continue;
+            const Item x = item(it);
+            T* dst;
+            if ((int)x.h < hq) {
+                dst = (T*)j.q_out.data + (tok0 + x.t) * j.q_out.token + (long)x.h * j.q_out.head;
+                if (PAGED && place[x.t].ignored) continue;
+            } else if (!PAGED)
+                dst = (T*)j.k_out.data + (tok0 + x.t) * j.k_out.token + (long)((int)x.h - hq) * j.k_out.head;
+            else {
+                const bool key = (int)x.h < hq + hk;
+                if (place[x.t].row < 0) continue;
+                dst = (T*)(key ? c.k : c.v) + place[x.t].row + (((long)((int)x.h - (key ? hq : hq + hk)) * c.dim) << c.page_shift);
             }
-            a = u;
-            b = v;
+            if (turns(x)) {
+                const float2* at = cs + x.t * n + x.piece * VE;
+                V y, z;
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    if (!j.adjacent || VE == 1) {
+                        const float p = widen(a[u].e[e]), q = widen(b[u].e[e]);
+                        narrow(p * at[e].x - q * at[e].y, y.e[e]);
+                        narrow(p * at[e].y + q * at[e].x, z.e[e]);
+                    } else if ((e & 1) == 0) {
+                        const int f = VE > 1 ? e + 1 : e;      // (there is one: VE is even here)
+                        const float2 s = at[e / 2], w = at[VE / 2 + e / 2];
+                        const float p = widen(a[u].e[e]), q = widen(a[u].e[f]), r = widen(b[u].e[e]), v = widen(b[u].e[f]);
+                        narrow(p * s.x - q * s.y, y.e[e]);
+                        narrow(p * s.y + q * s.x, y.e[f]);
+                        narrow(r * w.x - v * w.y, z.e[e]);
+                        narrow(r * w.y + v * w.x, z.e[f]);
+                    }
+                }
+                a[u] = y;
+                b[u] = z;
+            }
+            const int hi = second(x);
+            store_once<PAGED>(a[u], dst + first(x));
+            if (hi < j.dim) store_once<PAGED>(b[u], dst + hi);
         }
-        store_once(a, dst + lo);
-        if (two) store_once(b, dst + hi);
+        base += BATCH * THREADS;
+        if (base < total) fetch(base);
     }
     if (PAGED) {
         for (int i = tid; i < here * c.heads; i += THREADS) {
@@ -214,10 +241,13 @@ int vector_values(const RotaryJob& j)
     return ve;
 }
 
-// Tokens of a workgroup: as many as it has angles for, as long as there are workgroups for every compute unit left.
-int tokens_of_group(const RotaryJob& j)
+// Tokens of a workgroup: as many as its threads take in one batch and as it has angles for, as long as there are workgroups for
+// every compute unit left.
+int tokens_of_group(const RotaryJob& j, int pieces)
 {
-    int tt = j.pairs ? MAX_ANGLES / j.pairs : MAX_TOKENS;
+    const int items = (j.q.heads + j.k.heads + j.v.heads) * pieces, angles = j.pairs ? MAX_ANGLES / j.pairs : MAX_TOKENS;
+    int tt = BATCH * THREADS / items;
+    tt = tt < angles ? tt : angles;
     tt = tt < 1 ? 1 : (tt > MAX_TOKENS ? MAX_TOKENS : tt);
     while (tt > 1 && j.tokens / tt < 4L * device_units()) tt /= 2;
     return tt;
@@ -226,7 +256,7 @@ int tokens_of_group(const RotaryJob& j)
 template <bool PAGED>
 hipError_t launch(const RotaryJob& j, const Cache& c, int lengths, hipStream_t st)
 {
-    const int tt = tokens_of_group(j), ve = vector_values(j), pieces = (j.dim + 2 * ve - 1) / (2 * ve);
+    const int ve = vector_values(j), pieces = (j.dim + 2 * ve - 1) / (2 * ve), tt = tokens_of_group(j, pieces);
     const dim3 grid((unsigned)((j.tokens + tt - 1) / tt)), block(THREADS);
     if (lengths == LENGTHS_LAST && grid.x > 64) lengths = LENGTHS_LATER;
 #define CB_ROTARY(type, n) hipLaunchKernelGGL((rotary_kernel<type, n, PAGED>), grid, block, 0, st, j, c, tt, pieces, lengths)
