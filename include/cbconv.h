@@ -463,7 +463,7 @@ int cb_cache_append(const cb_cache *cache, const cb_rotary *rotary, int32_t n_to
  *   s_j = scale * q . k_j, capped: softcap * tanh(s_j / softcap) where softcap > 0;  out = sum_j e^(s_j) v_j / sum_j e^(s_j).
  * q->heads is a multiple of n_kv_heads; query head i reads key head i / (q->heads / n_kv_heads).  lse_dev (may be NULL): n_seq x
  * q->heads float32, ln of the sum.  A sequence without a token, or with scores of minus infinity alone, gives zeros and minus
- * infinity.  n_seq * capacity * (key heads times blocks of 16 of their query heads) stays below 2^39.  accumulate = 1 (weight_dev not NULL): weight becomes decay * weight + the sum over the query heads that read it of
+ * infinity.  n_seq * capacity * (key heads times blocks of 16 of their query heads) stays below 2^35.  accumulate = 1 (weight_dev not NULL): weight becomes decay * weight + the sum over the query heads that read it of
  * e^(s_j - lse), for every slot that holds a token.  The sums' order depends on lengths and sizes alone. */
 typedef struct {
     float scale, softcap;      /* finite; softcap >= 0, 0: none */

@@ -11,10 +11,13 @@
 // what P^T wants there, if the tokens of a tile are numbered to suit; no value changes lanes but for the maximum.  Keys and values come
 // from memory into registers as the matrix cores take them, whole rows by neighbouring lanes.
 //
-// Work is split over the length.  A unit is UNIT tokens of a (sequence, key head, block of query heads); the units of all of them,
-// in order, are dealt to the workgroups in equal runs, whatever the lengths, which the kernel reads itself.  A run's end in the middle of a
-// (sequence, head) leaves a part in the scratch buffer, and the workgroup that comes last joins the parts, in order.
+// Work is split over the length.  The tiles of all (sequence, key head, block of query heads), in order, are dealt to the workgroups in
+// equal runs, whatever the lengths, which the kernel reads itself, and a run to its wavefronts in the same way.  A wavefront goes through its
+// run by itself: what it has whole it finishes, and what begins or ends in the middle of something waits in LDS until all wavefronts are
+// through.  What begins or ends in the middle of something for the workgroup goes to the scratch buffer, and the workgroup that comes last
+// of those that share it joins the parts, in order.
 #include "cb_tokens.h"
+#include <cstdlib>
 
 namespace cb {
 
@@ -26,13 +29,13 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr float LOWEST = -3.402823466e38f;       // of a maximum, so that nothing is subtracted from minus infinity
 constexpr int ROWS = ATTEND_ROWS;
-constexpr int UNIT = 256;
 
 struct AttendArgs {
     AttendJob j;
     Cache c;
+    int rounds;                    // tiles a wavefront from which on a pair is split
     int group, blocks;             // query heads of a key head, blocks of ROWS of them
-    int q_aligned;
+    int q_aligned, out_aligned;    // to 16 bytes
     int* counters;
     float *parts, *lse, *scores;
     int pitch;                     // of a query head's scores
@@ -55,33 +58,32 @@ __device__ __forceinline__ float2 get(const float* at)
     return make_float2(__uint_as_float((unsigned)w), __uint_as_float((unsigned)(w >> 32)));
 }
 
-// The units of the sequences in order, and who has them.  All of it is the same for every lane of a wavefront.
-struct Units {
+// The tiles of the sequences in order.  All of it is the same for every lane of a wavefront.
+struct Tiles {
     const int32_t* lengths;
     int seqs, capacity, per_seq;       // per_seq: (key head, block) pairs of a sequence
-    __device__ int of(int len) const { return len > UNIT ? (len + UNIT - 1) / UNIT : 1; }
-    __device__ int at(int s) const { return of(clamp_length(lengths[s], capacity)) * per_seq; }
-    __device__ int total() const
+    int tokens, enough;                // of a tile; tiles of a pair that keep a workgroup busy
+    __device__ int of(int len) const { return len > tokens ? (len + tokens - 1) / tokens : 1; }
+    // all tiles, and how many workgroups are worth while: a pair is split where each part has `enough`
+    __device__ void total(unsigned* tiles, unsigned* groups) const
     {
         const int lane = threadIdx.x & 63;
-        int sum = 0;
-        for (int s = lane; s < seqs; s += 64) sum += at(s);
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-        return __builtin_amdgcn_readfirstlane(sum);
+        int sum = 0, worth = 0;
+        for (int s = lane; s < seqs; s += 64) {
+            const int n = of(clamp_length(lengths[s], capacity));
+            sum += n;
+            worth += n < 2 * enough ? 1 : n / enough;
+        }
+        *tiles = (unsigned)__builtin_amdgcn_readlane(wave_scan(sum), 63) * per_seq;
+        *groups = (unsigned)__builtin_amdgcn_readlane(wave_scan(worth), 63) * per_seq;
     }
-    // the sequence that unit u belongs to, and its first unit
+    // the sequence that tile u belongs to, and its first tile
     __device__ int find(int u, int* first) const
     {
         const int lane = threadIdx.x & 63;
         int before = 0;
         for (int s0 = 0; s0 < seqs; s0 += 64) {
-            int sum = s0 + lane < seqs ? at(s0 + lane) : 0;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const int up = __shfl_up(sum, d);
-                if (lane >= d) sum += up;
-            }
+            const int sum = wave_scan(s0 + lane < seqs ? of(clamp_length(lengths[s0 + lane], capacity)) * per_seq : 0);
             const unsigned long long past = __ballot(before + sum > u);
             if (past) {
                 const int at = __builtin_ctzll(past);
@@ -95,12 +97,12 @@ struct Units {
     }
 };
 
-// n units dealt to w workgroups: the first n % w get one more than the others.
+// n tiles dealt to w: the first n % w get one more than the others.
 struct Deal {
     unsigned each, more;
     __device__ Deal(unsigned n, unsigned w) : each(n / w), more(n % w) {}
     __device__ unsigned first(unsigned g) const { return g * each + (g < more ? g : more); }
-    __device__ unsigned owner(unsigned u) const
+    __device__ unsigned owner(unsigned u) const      // (each is not 0)
     {
         const unsigned big = more * (each + 1);
         return u < big ? u / (each + 1) : more + (u - big) / each;
@@ -110,7 +112,7 @@ struct Deal {
 // How a type's tiles look.  PE: consecutive values of a row that a lane takes of V, NP such pieces 16 * PE apart.
 template <typename T, int DP> struct Tile;
 template <int DP> struct Tile<uint16_t, DP> {
-    static constexpr int WAVES = DP == 256 ? 4 : 8;      // of a workgroup: as many as its registers have room for
+    static constexpr int WAVES = DP == 256 ? 4 : 8;
     static constexpr int TOKENS = 32, PE = DP == 64 ? 4 : 8, NP = DP / (16 * PE);
     static constexpr int KSTEPS = DP / 32;       // of S^T: 32 values of a head a step
 };
@@ -121,9 +123,9 @@ template <int DP> struct Tile<float, DP> {
 };
 
 // A wavefront's pages: lane x has that of its sub-tile x (16 tokens) of the next 64.
-template <int SUB, int WAVES> __device__ __forceinline__ int load_pages(const int32_t* table, int shift, int n_pages, int tile, int len)
+template <int SUB> __device__ __forceinline__ int load_pages(const int32_t* table, int shift, int n_pages, int tile, int len)
 {
-    const int lane = threadIdx.x & 63, tok = (tile + lane / SUB * WAVES) * SUB * 16 + lane % SUB * 16;
+    const int tok = (tile * SUB + (int)(threadIdx.x & 63)) * 16;
     int page = -1;
     if (tok < len) page = table[tok >> shift];
     return (unsigned)page < (unsigned)n_pages ? page : -1;
@@ -137,83 +139,80 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
     constexpr bool HALF = sizeof(T) == 2;
     typedef Tile<T, DP> TL;
     constexpr int WAVES = TL::WAVES, THREADS = WAVES * 64, SUB = TL::TOKENS / 16, NP = TL::NP, PE = TL::PE, KSTEPS = TL::KSTEPS;
-    constexpr int ROUNDS = UNIT / (WAVES * TL::TOKENS);                // tiles of a wavefront in a unit
     constexpr int DW = PE * (int)sizeof(T) / 4;                        // 32-bit words of a piece
     typedef uint32_t piece_t __attribute__((ext_vector_type(DW)));
     typedef uint32_t key_t __attribute__((ext_vector_type(4)));
-    __shared__ float s_o[WAVES][ROWS][DP + 4];
-    __shared__ float s_m[WAVES][ROWS], s_l[WAVES][ROWS];
-    __shared__ int s_last;
+    // a wavefront's two parts: of what begins before its run, and of what goes on behind it
+    __shared__ __align__(16) float s_o[2 * WAVES][ROWS][DP + 4];
+    __shared__ float s_m[2 * WAVES][ROWS], s_l[2 * WAVES][ROWS];
+    __shared__ int s_first[2 * WAVES];                                 // first tile of the pair that a part belongs to, -1: no part
+    __shared__ int s_seq[2 * WAVES], s_pair[2 * WAVES], s_tiles[2 * WAVES];
+    __shared__ int s_last[2];
 
     const Cache& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
     const int D = c.dim, per_seq = c.heads * a.blocks;
-    const Units units{c.lengths, c.seqs, c.capacity, per_seq};
-    const unsigned total = units.total(), groups = total < gridDim.x ? total : gridDim.x;
+    const Tiles tiles{c.lengths, c.seqs, c.capacity, per_seq, TL::TOKENS, a.rounds * WAVES};
+    unsigned total, groups;
+    tiles.total(&total, &groups);
+    groups = groups < gridDim.x ? groups : gridDim.x;
     if (blockIdx.x >= groups) return;
     const Deal deal(total, groups);
-    int u = deal.first(blockIdx.x);
-    const int end = deal.first(blockIdx.x + 1);
+    const int run = deal.first(blockIdx.x);
+    const Deal own(deal.first(blockIdx.x + 1) - run, WAVES);
+    int u = run + own.first(wave);
+    const int end = run + own.first(wave + 1);
+    if (lane < 2) s_first[2 * wave + lane] = -1;
 
-    int first;
-    int seq = units.find(u, &first);
-    while (u < end && seq < c.seqs) {
-        const int len = clamp_length(c.lengths[seq], c.capacity), nu = units.of(len);
-        const int pair = (unsigned)(u - first) / (unsigned)nu, from = u - first - pair * nu;
-        const int to = nu - from < end - u ? nu : from + (end - u);
-        const int h = (unsigned)pair / (unsigned)a.blocks, blk = pair - h * a.blocks;
-        const int row0 = blk * ROWS, rows = a.group - row0 < ROWS ? a.group - row0 : ROWS;
-        const int32_t* table = c.table + (long)seq * c.max_pages;
-
-        // this wavefront's tiles: t, t + WAVES, ... below t1
-        int t = from * (ROUNDS * WAVES) + wave;
-        const int t1 = to * (ROUNDS * WAVES) < (len + TL::TOKENS - 1) / TL::TOKENS ? to * (ROUNDS * WAVES) : (len + TL::TOKENS - 1) / TL::TOKENS;
-        int pages = load_pages<SUB, WAVES>(table, c.page_shift, c.n_pages, t, len), ahead = -1, used = 0;
-        if (t + 64 / SUB * WAVES < t1) ahead = load_pages<SUB, WAVES>(table, c.page_shift, c.n_pages, t + 64 / SUB * WAVES, len);
-
-        // this lane's part of the query heads: head l16, values 32 * i + 8 * quad .. (or 16 * i + 4 * quad ..)
-        key_t q[KSTEPS];
-        {
-            const T* src = (const T*)a.j.q.data + (long)seq * a.j.q.token + (long)(h * a.group + row0 + l16) * a.j.q.head;
-            constexpr int E = 16 / (int)sizeof(T);
+    // A run is worked through a pair (sequence, head, block) at a time: those of its tiles that fall into one.
+    struct Stretch {
+        int seq, first, len, n, pair, from, to, h, row0, rows;        // first: tile of the sequence's first pair; n: tiles of a pair
+    };
+    auto stretch = [&](int seq, int first) {
+        Stretch x;
+        x.seq = seq;
+        x.first = first;
+        x.len = clamp_length(c.lengths[seq], c.capacity);
+        x.n = tiles.of(x.len);
+        x.pair = (unsigned)(u - first) / (unsigned)x.n;
+        x.from = u - first - x.pair * x.n;
+        x.to = x.n - x.from < end - u ? x.n : x.from + (end - u);
+        x.h = (unsigned)x.pair / (unsigned)a.blocks;
+        x.row0 = (x.pair - x.h * a.blocks) * ROWS;
+        x.rows = a.group - x.row0 < ROWS ? a.group - x.row0 : ROWS;
+        return x;
+    };
+    // tile: where its sub-tiles' rows are (in values), how many tokens they hold
+    struct Where { long at[SUB]; int left[SUB]; };
+    key_t q[KSTEPS], k[SUB][KSTEPS];
+    piece_t v[SUB][4][NP];
+    int t = 0, t1 = 0, pages = -1, ahead = -1, used = 0;       // tiles t .. t1 - 1, their pages
+    Where here, next;
+    auto find = [&](const Stretch& x, int tile, int slot) {
+        Where w;
 #pragma unroll
-            for (int i = 0; i < KSTEPS; ++i) {
-                const int d = (4 * i + quad) * E;
-                q[i] = key_t(0);
-                if (l16 < rows && d < D) {
-                    if (a.q_aligned) q[i] = *reinterpret_cast<const key_t*>(src + d);
-                    else {
-                        T e[E];
-#pragma unroll
-                        for (int x = 0; x < E; ++x) e[x] = src[d + x];
-                        __builtin_memcpy(&q[i], e, 16);
-                    }
-                }
-            }
+        for (int s = 0; s < SUB; ++s) {
+            const int tok = tile * TL::TOKENS + 16 * s, page = __builtin_amdgcn_readlane(pages, slot * SUB + s);
+            w.left[s] = page >= 0 ? (x.len - tok < 16 ? x.len - tok : 16) : 0;
+            w.at[s] = page >= 0 ? ((((long)page * c.heads + x.h) << c.page_shift) + (tok & ((1 << c.page_shift) - 1))) * D : 0;
         }
-        float m = LOWEST, l = 0.0f;
-        f32x4 o[NP * PE];
+        return w;
+    };
+    auto full = [&](const Where& w) {
+        bool f = D == DP;
 #pragma unroll
-        for (int i = 0; i < NP * PE; ++i) o[i] = f32x4{0, 0, 0, 0};
-
-        key_t k[SUB][KSTEPS];
-        piece_t v[SUB][4][NP];
-        // tile x: where its sub-tiles' rows are (in values), how many tokens they hold
-        struct Where { long at[SUB]; int left[SUB]; };
-        auto find = [&](int x, int slot) {
-            Where w;
+        for (int s = 0; s < SUB; ++s) f = f && w.left[s] == 16;
+        return f;
+    };
+    auto load_k = [&](const Where& w) {
+        const bool all = full(w);
 #pragma unroll
-            for (int s = 0; s < SUB; ++s) {
-                const int tok = x * TL::TOKENS + 16 * s, page = __builtin_amdgcn_readlane(pages, slot * SUB + s);
-                w.left[s] = page >= 0 ? (len - tok < 16 ? len - tok : 16) : 0;
-                w.at[s] = page >= 0 ? ((((long)page * c.heads + h) << c.page_shift) + (tok & ((1 << c.page_shift) - 1))) * D : 0;
-            }
-            return w;
-        };
-        auto load_k = [&](const Where& w) {
+        for (int s = 0; s < SUB; ++s) {
+            const T* src = (const T*)c.k + w.at[s] + l16 * D;
+            if (all) {
 #pragma unroll
-            for (int s = 0; s < SUB; ++s) {
-                const T* src = (const T*)c.k + w.at[s] + l16 * D;
+                for (int i = 0; i < KSTEPS; ++i) k[s][i] = load_once<key_t>(src + (4 * i + quad) * (16 / (int)sizeof(T)));
+            } else {
 #pragma unroll
                 for (int i = 0; i < KSTEPS; ++i) {
                     const int d = (4 * i + quad) * (16 / (int)sizeof(T));
@@ -221,11 +220,19 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                     if (l16 < w.left[s] && d < D) k[s][i] = load_once<key_t>(src + d);
                 }
             }
-        };
-        auto load_v = [&](const Where& w) {
+        }
+    };
+    auto load_v = [&](const Where& w) {
+        const bool all = full(w);
 #pragma unroll
-            for (int s = 0; s < SUB; ++s) {
-                const T* src = (const T*)c.v + w.at[s] + 4 * quad * D;
+        for (int s = 0; s < SUB; ++s) {
+            const T* src = (const T*)c.v + w.at[s] + 4 * quad * D;
+            if (all) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) v[s][r][p] = load_once<piece_t>(src + r * D + (16 * p + l16) * PE);
+            } else {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -235,14 +242,76 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                         if (4 * quad + r < w.left[s] && d < D) v[s][r][p] = load_once<piece_t>(src + r * D + d);
                     }
             }
-        };
-        Where here, next;
+        }
+    };
+    // what a stretch begins with: its pages, query heads, and first tile
+    auto begin = [&](const Stretch& x) {
+        const int32_t* table = c.table + (long)x.seq * c.max_pages;
+        t = x.from;
+        t1 = x.len > 0 ? x.to : t;
+        used = 0;
+        pages = load_pages<SUB>(table, c.page_shift, c.n_pages, t, x.len);
+        ahead = -1;
+        if (t + 64 / SUB < t1) ahead = load_pages<SUB>(table, c.page_shift, c.n_pages, t + 64 / SUB, x.len);
+        // this lane's part of the query heads: head l16, values 32 * i + 8 * quad .. (or 16 * i + 4 * quad ..)
+        const T* src = (const T*)a.j.q.data + (long)x.seq * a.j.q.token + (long)(x.h * a.group + x.row0 + l16) * a.j.q.head;
+        constexpr int E = 16 / (int)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < KSTEPS; ++i) {
+            const int d = (4 * i + quad) * E;
+            q[i] = key_t(0);
+            if (l16 < x.rows && d < D) {
+                if (a.q_aligned) q[i] = *reinterpret_cast<const key_t*>(src + d);
+                else {
+                    T e[E];
+#pragma unroll
+                    for (int y = 0; y < E; ++y) e[y] = src[d + y];
+                    __builtin_memcpy(&q[i], e, 16);
+                }
+            }
+        }
         if (t < t1) {
-            here = find(t, 0);
+            here = find(x, t, 0);
             load_k(here);
             load_v(here);
         }
-        for (; t < t1; t += WAVES) {
+    };
+
+    // row, values d and d + 1 of a pair's result: x and y over L
+    auto finish = [&](int seq, int head, int d, float M, float L, float x, float y) {
+        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+        if (d < D) {
+            T* out = (T*)a.j.out.data + (long)seq * a.j.out.token + (long)head * a.j.out.head + d;
+            T e0, e1;
+            narrow(x * inv, e0);
+            narrow(y * inv, e1);
+            out[0] = e0;
+            out[1] = e1;
+        }
+        if (d == 0) {
+            const float z = L == 0.0f ? -__builtin_inff() : M + __builtin_amdgcn_logf(L) * LN2;
+            if (a.j.lse) a.j.lse[(long)seq * a.j.q.heads + head] = z;
+            a.lse[(long)seq * a.j.q.heads + head] = z;
+        }
+    };
+
+    Stretch x;
+    bool over = true;
+    if (u < end) {
+        int first;
+        const int seq = tiles.find(u, &first);
+        if (seq < c.seqs) {
+            over = false;
+            x = stretch(seq, first);
+            begin(x);
+        }
+    }
+    while (!over) {
+        float m = LOWEST, l = 0.0f;
+        f32x4 o[NP * PE];
+#pragma unroll
+        for (int i = 0; i < NP * PE; ++i) o[i] = f32x4{0, 0, 0, 0};
+        for (; t < t1; ++t) {
             // scores of tokens 16 * s + 4 * quad + r for query head l16
             f32x4 sc[SUB];
 #pragma unroll
@@ -260,14 +329,14 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                 }
             }
             // the next tile's keys come while this one's weights are made, its values while the next one's scores are
-            const bool more = t + WAVES < t1;
+            const bool more = t + 1 < t1;
             if (more) {
                 if (++used == 64 / SUB) {
                     used = 0;
                     pages = ahead;
-                    if (t + (1 + 64 / SUB) * WAVES < t1) ahead = load_pages<SUB, WAVES>(table, c.page_shift, c.n_pages, t + (1 + 64 / SUB) * WAVES, len);
+                    if (t + 1 + 64 / SUB < t1) ahead = load_pages<SUB>(c.table + (long)x.seq * c.max_pages, c.page_shift, c.n_pages, t + 1 + 64 / SUB, x.len);
                 }
-                next = find(t + WAVES, used);
+                next = find(x, t + 1, used);
                 load_k(next);
             }
             float top = LOWEST;
@@ -275,14 +344,14 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
             for (int s = 0; s < SUB; ++s)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    float x = sc[s][r] * a.j.scale;
-                    if (a.j.softcap > 0.0f) x = a.j.softcap * tanhf(x / a.j.softcap);
-                    x = 4 * quad + r < here.left[s] ? x : -__builtin_inff();
-                    sc[s][r] = x;
-                    top = fmaxf(top, x);
+                    float y = sc[s][r] * a.j.scale;
+                    if (a.j.softcap > 0.0f) y = a.j.softcap * tanhf(y / a.j.softcap);
+                    y = 4 * quad + r < here.left[s] ? y : -__builtin_inff();
+                    sc[s][r] = y;
+                    top = fmaxf(top, y);
                 }
-            if (a.scores && l16 < rows) {
-                float* to_scores = a.scores + ((long)seq * a.j.q.heads + h * a.group + row0 + l16) * a.pitch + t * TL::TOKENS + 4 * quad;
+            if (a.scores && l16 < x.rows) {
+                float* to_scores = a.scores + ((long)x.seq * a.j.q.heads + x.h * a.group + x.row0 + l16) * a.pitch + t * TL::TOKENS + 4 * quad;
 #pragma unroll
                 for (int s = 0; s < SUB; ++s)
                     if (t * TL::TOKENS + 16 * s < a.pitch) *reinterpret_cast<f32x4*>(to_scores + 16 * s) = sc[s];
@@ -345,111 +414,199 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
 
-        // join the wavefronts: lane has o of query head l16, values (16 * p + 4 * quad + r) * PE + e
-        __syncthreads();
-        if (quad == 0) { s_m[wave][l16] = m; s_l[wave][l16] = l; }
-        if (l16 < rows) {
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int e = 0; e < PE; ++e) s_o[wave][l16][(16 * p + 4 * quad + r) * PE + e] = o[p * PE + e][r];
+        // the next stretch begins to come while this one is put away
+        const Stretch done = x;
+        u += done.to - done.from;
+        const bool same = u - done.first < done.n * per_seq;
+        const int seq = same ? done.seq : done.seq + 1;
+        over = u >= end || seq >= c.seqs;
+        if (!over) {
+            x = stretch(seq, same ? done.first : done.first + done.n * per_seq);
+            begin(x);
         }
-        __syncthreads();
-
-        const long q_head = (long)seq * a.j.q.heads + h * a.group + row0;
-        // row, values d and d + 1: x and y over L
-        auto finish = [&](int row, int d, float M, float L, float x, float y) {
-            const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-            if (d < D) {
-                T* out = (T*)a.j.out.data + (long)seq * a.j.out.token + (long)(h * a.group + row0 + row) * a.j.out.head + d;
-                T e0, e1;
-                narrow(x * inv, e0);
-                narrow(y * inv, e1);
-                out[0] = e0;
-                out[1] = e1;
-            }
-            if (d == 0) {
-                const float z = L == 0.0f ? -__builtin_inff() : M + __builtin_amdgcn_logf(L) * LN2;
-                if (a.j.lse) a.j.lse[q_head + row] = z;
-                a.lse[q_head + row] = z;
-            }
-        };
-        // what the wavefronts have of row, values d and d + 1
-        auto join = [&](int row, int d, float* M, float* L, float* x, float* y) {
-            *M = LOWEST;
-            *L = *x = *y = 0.0f;
+        // lane has o of query head l16, values (16 * p + 4 * quad + r) * PE + e: runs of 4 * PE values
+        if (done.from == 0 && done.to == done.n) {
+            const int head = done.h * a.group + done.row0 + l16;
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            if (l16 < done.rows) {
+                T* out = (T*)a.j.out.data + (long)done.seq * a.j.out.token + (long)head * a.j.out.head;
+                constexpr int E = 16 / (int)sizeof(T);
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) *M = fmaxf(*M, s_m[w][row]);
+                for (int p = 0; p < NP; ++p)
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                const float f = exp_of(s_m[w][row] - *M);
-                *L += f * s_l[w][row];
-                *x += f * s_o[w][row][d];
-                *y += f * s_o[w][row][d + 1];
-            }
-        };
-        const bool whole = from == 0 && to == nu;
-        float* mine = a.parts + (2L * blockIdx.x + (from == 0 ? 1 : 0)) * part_floats<DP>();
-        for (int i = 2 * tid; i < rows * DP; i += 2 * THREADS) {
-            const int row = i / DP, d = i % DP;
-            float M, L, x, y;
-            join(row, d, &M, &L, &x, &y);
-            if (whole) finish(row, d, M, L, x, y);
-            else {
-                put(mine + 2 * ROWS + i, x, y);
-                if (d == 0) put(mine + 2 * row, M, L);
-            }
-        }
-        if (!whole) {
-            __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): this wavefront's stores are where every compute unit sees them
-            __syncthreads();
-            // the workgroups that share this pair; the first of them has no other pair that goes on behind it
-            const unsigned u0 = first + pair * nu, w0 = deal.owner(u0), w1 = deal.owner(u0 + nu - 1);
-            if (tid == 0) {
-                s_last = __hip_atomic_fetch_add(a.counters + w0, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)(w1 - w0);
-                if (s_last) __hip_atomic_store(a.counters + w0, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-            __syncthreads();
-            if (s_last) {
-                // each wavefront takes every WAVES-th part, in order; then the wavefronts are joined as before
-                for (int i = 2 * lane; i < rows * DP; i += 128) {
-                    const int row = i / DP, d = i % DP;
-                    float M = LOWEST, L = 0.0f, x = 0.0f, y = 0.0f;
-                    for (unsigned w = w0 + wave; w <= w1; w += 4 * WAVES) {
-                        float2 ml[4], xy[4];
+                    for (int y = 0; y < 4 * PE / E; ++y) {
+                        const int d = (16 * p + 4 * quad) * PE + y * E;
+                        T w[E];
 #pragma unroll
-                        for (int n = 0; n < 4; ++n) {
-                            const unsigned g = w + n * WAVES;
-                            const float* part = a.parts + (2L * g + (g == w0 ? 1 : 0)) * part_floats<DP>();
-                            ml[n] = make_float2(LOWEST, 0.0f);
-                            xy[n] = make_float2(0.0f, 0.0f);
-                            if (g <= w1) { ml[n] = get(part + 2 * row); xy[n] = get(part + 2 * ROWS + i); }
-                        }
+                        for (int z = 0; z < E; ++z) narrow(o[p * PE + (y * E + z) % PE][(y * E + z) / PE] * inv, w[z]);
+                        if (d < D) {
+                            if (a.out_aligned) {
+                                key_t word;
+                                __builtin_memcpy(&word, w, 16);
+                                *reinterpret_cast<key_t*>(out + d) = word;
+                            } else
 #pragma unroll
-                        for (int n = 0; n < 4; ++n) {
-                            const float top = fmaxf(M, ml[n].x), f = exp_of(M - top), g = exp_of(ml[n].x - top);
-                            M = top;
-                            L = f * L + g * ml[n].y;
-                            x = f * x + g * xy[n].x;
-                            y = f * y + g * xy[n].y;
+                                for (int z = 0; z < E; ++z) out[d + z] = w[z];
                         }
                     }
-                    s_o[wave][row][d] = x;
-                    s_o[wave][row][d + 1] = y;
-                    if (d == 0) { s_m[wave][row] = M; s_l[wave][row] = L; }
+                if (quad == 0) {
+                    const float z = l == 0.0f ? -__builtin_inff() : m + __builtin_amdgcn_logf(l) * LN2;
+                    if (a.j.lse) a.j.lse[(long)done.seq * a.j.q.heads + head] = z;
+                    a.lse[(long)done.seq * a.j.q.heads + head] = z;
                 }
-                __syncthreads();
-                for (int i = 2 * tid; i < rows * DP; i += 2 * THREADS) {
-                    float M, L, x, y;
-                    join(i / DP, i % DP, &M, &L, &x, &y);
-                    finish(i / DP, i % DP, M, L, x, y);
+            }
+        } else {
+            const int slot = 2 * wave + (done.from == 0 ? 1 : 0);
+            if (quad == 0) { s_m[slot][l16] = m; s_l[slot][l16] = l; }
+            if (l16 < done.rows) {
+#pragma unroll
+                for (int p = 0; p < NP; ++p)
+#pragma unroll
+                    for (int y = 0; y < PE; ++y) {
+                        f32x4 w;
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) w[z] = o[p * PE + (4 * y + z) % PE][(4 * y + z) / PE];
+                        *reinterpret_cast<f32x4*>(&s_o[slot][l16][(16 * p + 4 * quad) * PE + 4 * y]) = w;
+                    }
+            }
+            if (lane == 0) {
+                s_first[slot] = done.first + done.pair * done.n;
+                s_seq[slot] = done.seq;
+                s_pair[slot] = done.pair;
+                s_tiles[slot] = done.n;
+            }
+        }
+    }
+    __syncthreads();
+
+    // The parts of a pair: the first one a part that goes on behind its wavefront's run (or the workgroup's first part, of what begins before its
+    // run), the others the first parts of the wavefronts behind.  Wavefronts without tiles are behind all others.
+    struct Chain { int slot, wave, parts, seq, first, n, pair, head0, rows; };
+    auto chain = [&](int slot) {
+        Chain x;
+        x.slot = slot;
+        x.first = __builtin_amdgcn_readfirstlane(s_first[slot]);
+        x.seq = __builtin_amdgcn_readfirstlane(s_seq[slot]);
+        x.pair = __builtin_amdgcn_readfirstlane(s_pair[slot]);
+        x.n = __builtin_amdgcn_readfirstlane(s_tiles[slot]);
+        x.wave = slot >> 1;
+        x.parts = 1;
+        while (x.wave + x.parts < WAVES && __builtin_amdgcn_readfirstlane(s_first[2 * (x.wave + x.parts)]) == x.first) ++x.parts;
+        const int h = (unsigned)x.pair / (unsigned)a.blocks, row0 = (x.pair - h * a.blocks) * ROWS;
+        x.head0 = h * a.group + row0;
+        x.rows = a.group - row0 < ROWS ? a.group - row0 : ROWS;
+        return x;
+    };
+    // slots s0, s0 + step, ... of row, values d and d + 1
+    auto join = [&](int s0, int rest, int parts, int row, int d, float* M, float* L, float* x, float* y) {
+        *M = s_m[s0][row];
+        for (int p = 1; p < parts; ++p) *M = fmaxf(*M, s_m[rest + 2 * p][row]);
+        *L = *x = *y = 0.0f;
+        for (int p = 0; p < parts; ++p) {
+            const int s = p == 0 ? s0 : rest + 2 * p;
+            const float f = exp_of(s_m[s][row] - *M);
+            const float2 v = *reinterpret_cast<const float2*>(&s_o[s][row][d]);
+            *L += f * s_l[s][row];
+            *x += f * v.x;
+            *y += f * v.y;
+        }
+    };
+    bool mine[2] = {false, false};                             // parts of this workgroup that others have to do with
+    const int run_end = deal.first(blockIdx.x + 1);
+    for (int slot = 0; slot < 2 * WAVES; ++slot) {
+        // a part that begins before its wavefront's run belongs to the chain of an earlier one, but for the workgroup's first
+        if ((slot > 0 && (slot & 1) == 0) || s_first[slot] < 0) continue;
+        const Chain x = chain(slot);
+        const bool whole = x.first >= run && x.first + x.n <= run_end;
+        const int w = x.first < run ? 0 : 1;
+        float* part = a.parts + (2L * blockIdx.x + w) * part_floats<DP>();
+        for (int i = 2 * tid; i < x.rows * DP; i += 2 * THREADS) {
+            const int row = i / DP, d = i % DP;
+            float M, L, y, z;
+            join(x.slot, 2 * x.wave, x.parts, row, d, &M, &L, &y, &z);
+            if (whole) finish(x.seq, x.head0 + row, d, M, L, y, z);
+            else {
+                put(part + 2 * ROWS + i, y, z);
+                if (d == 0) put(part + 2 * row, M, L);
+            }
+        }
+        if (!whole) mine[w] = true;
+    }
+    if (!mine[0] && !mine[1]) return;
+    __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): this wavefront's stores are where every compute unit sees them
+    __syncthreads();
+    // the workgroups that share a pair count themselves at its first one's counter; that one has no other pair that goes on behind it
+    int slots[2] = {0, 0};
+    unsigned w0[2] = {0, 0}, w1[2] = {0, 0};
+    for (int w = 0; w < 2; ++w)
+        if (mine[w]) {
+            int slot = 0;                        // the workgroup's first part, or the last one that goes on
+            if (w == 1)
+                for (int y = 0; y < WAVES; ++y)
+                    if (s_first[2 * y + 1] >= 0) slot = 2 * y + 1;
+            slots[w] = slot;
+            const unsigned u0 = __builtin_amdgcn_readfirstlane(s_first[slot]);
+            w0[w] = deal.owner(u0);
+            w1[w] = deal.owner(u0 + __builtin_amdgcn_readfirstlane(s_tiles[slot]) - 1);
+            if (tid == w) {
+                int* counter = a.counters + w0[w];
+                s_last[w] = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)(w1[w] - w0[w]);
+                if (s_last[w]) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+        }
+    __syncthreads();
+    for (int w = 0; w < 2; ++w) {
+        if (!mine[w] || !s_last[w]) continue;
+        const Chain x = chain(slots[w]);
+        const int rows = x.rows;
+        __syncthreads();                         // (everyone has read what the parts are of)
+        // Each wavefront takes every WAVES-th part, in order; then the wavefronts are joined.  A part is a trip to memory past
+        // the caches: four parts of four values a lane are on their way at once.
+        for (int i0 = 2 * lane; i0 < rows * DP; i0 += 512) {
+            float M[4], L[4], y[4], z[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { M[k] = LOWEST; L[k] = y[k] = z[k] = 0.0f; }
+            for (unsigned g0 = w0[w] + wave; g0 <= w1[w]; g0 += 4 * WAVES) {
+                float2 ml[4][4], xy[4][4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const unsigned g = g0 + n * WAVES;
+                    const float* part = a.parts + (2L * g + (g == w0[w] ? 1 : 0)) * part_floats<DP>();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int i = i0 + 128 * k;
+                        ml[n][k] = make_float2(LOWEST, 0.0f);
+                        xy[n][k] = make_float2(0.0f, 0.0f);
+                        if (g <= w1[w] && i < rows * DP) { ml[n][k] = get(part + 2 * (i / DP)); xy[n][k] = get(part + 2 * ROWS + i); }
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float top = fmaxf(M[k], ml[n][k].x), f = exp_of(M[k] - top), g = exp_of(ml[n][k].x - top);
+                        M[k] = top;
+                        L[k] = f * L[k] + g * ml[n][k].y;
+                        y[k] = f * y[k] + g * xy[n][k].x;
+                        z[k] = f * z[k] + g * xy[n][k].y;
+                    }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int i = i0 + 128 * k, row = i / DP, d = i % DP;
+                if (i < rows * DP) {
+                    *reinterpret_cast<float2*>(&s_o[2 * wave][row][d]) = make_float2(y[k], z[k]);
+                    if (d == 0) { s_m[2 * wave][row] = M[k]; s_l[2 * wave][row] = L[k]; }
                 }
             }
         }
-        u += to - from;
-        if (u - first >= nu * per_seq) { first += nu * per_seq; ++seq; }
+        __syncthreads();
+        for (int i = 2 * tid; i < rows * DP; i += 2 * THREADS) {
+            float M, L, y, z;
+            join(0, 0, WAVES, i / DP, i % DP, &M, &L, &y, &z);
+            finish(x.seq, x.head0 + i / DP, i % DP, M, L, y, z);
+        }
+        __syncthreads();
     }
 }
 
@@ -478,8 +635,8 @@ __global__ __launch_bounds__(256) void weight_kernel(const AttendArgs a)
 
 bool attend_fits(const Cache& c, int q_heads)
 {
-    const unsigned long long blocks = (unsigned)(q_heads / c.heads + ROWS - 1) / ROWS, units = (unsigned)(c.capacity + UNIT - 1) / UNIT;
-    return (unsigned long long)c.seqs * c.heads * blocks * units < (1ull << 31);
+    const unsigned long long blocks = (unsigned)(q_heads / c.heads + ROWS - 1) / ROWS, tiles = (unsigned)c.capacity / 16;
+    return (unsigned long long)c.seqs * c.heads * blocks * tiles < (1ull << 31);
 }
 
 hipError_t launch_attend(const AttendJob& j, const Cache& c, hipStream_t st)
@@ -498,8 +655,10 @@ hipError_t launch_attend(const AttendJob& j, const Cache& c, hipStream_t st)
     a.scores = j.accumulate ? reinterpret_cast<float*>(c.scratch + plan.scores) : nullptr;
     a.pitch = c.capacity;
     const int dp = c.dim <= 64 ? 64 : (c.dim <= 128 ? 128 : 256);
-    // one workgroup a compute unit, no more than there can be units
-    const long most = (long)c.seqs * c.heads * a.blocks * ((c.capacity + UNIT - 1) / UNIT);
+    a.out_aligned = (uintptr_t)j.out.data % 16 == 0 && j.out.token % align == 0 && j.out.head % align == 0;
+    const char* E = getenv("CB_R"); a.rounds = E ? atoi(E) : 2;
+    // one workgroup a compute unit, no more than there can be tiles
+    const long most = (long)c.seqs * c.heads * a.blocks * (c.capacity / (c.bf16 ? 32 : 16) + 1);
     const long want = device_units();
     const int groups = (int)(most < want ? most : (want < MAX_GROUPS ? want : MAX_GROUPS));
 #define CB_ATTEND(type, d) hipLaunchKernelGGL((attend_kernel<type, d>), dim3(groups), dim3(Tile<type, d>::WAVES * 64), 0, st, a)
