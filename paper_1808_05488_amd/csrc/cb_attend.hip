@@ -11,13 +11,13 @@
 // what P^T wants there, if the tokens of a tile are numbered to suit; no value changes lanes but for the maximum.  Keys and values come
 // from memory into registers as the matrix cores take them, whole rows by neighbouring lanes.
 //
-// Work is split over the length.  The tiles of all (sequence, key head, block of query heads), in order, are dealt to the workgroups in
-// equal runs, whatever the lengths, which the kernel reads itself, and a run to its wavefronts in the same way.  A wavefront goes through its
-// run by itself: what it has whole it finishes, and what begins or ends in the middle of something waits in LDS until all wavefronts are
-// through.  What begins or ends in the middle of something for the workgroup goes to the scratch buffer, and the workgroup that comes last
-// of those that share it joins the parts, in order.
+// Work is split over the length, whatever the lengths, which the kernel reads itself.  Where there are workgroups enough, every pair (sequence,
+// key head, block of query heads) has its own, more of them the longer it is; where there are not, the tiles of all pairs, in order, are dealt to
+// the workgroups in equal runs.  A run is dealt to the wavefronts in the same way.  A wavefront goes through its part by itself: what it has
+// whole it finishes, and what begins or ends in the middle of something waits in LDS until all wavefronts are through.  What
+// begins or ends in the middle of something for the workgroup goes to the scratch buffer, and the workgroup that comes last of those that
+// share it joins the parts, in order.
 #include "cb_tokens.h"
-#include <cstdlib>
 
 namespace cb {
 
@@ -29,11 +29,13 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr float LOWEST = -3.402823466e38f;       // of a maximum, so that nothing is subtracted from minus infinity
 constexpr int ROWS = ATTEND_ROWS;
+// Tiles of a wavefront that are worth a workgroup of their own: a part more costs its way through memory and the join.  (Five sequences of 1 - 9 001
+// tokens in float32: 25.8 us with 1, 22.6 with 2, 28.4 with 4; long ones have enough either way.)
+constexpr int SPLIT_TILES = 2;
 
 struct AttendArgs {
     AttendJob j;
     Cache c;
-    int rounds;                    // tiles a wavefront from which on a pair is split
     int group, blocks;             // query heads of a key head, blocks of ROWS of them
     int q_aligned, out_aligned;    // to 16 bytes
     int* counters;
@@ -64,26 +66,28 @@ struct Tiles {
     int seqs, capacity, per_seq;       // per_seq: (key head, block) pairs of a sequence
     int tokens, enough;                // of a tile; tiles of a pair that keep a workgroup busy
     __device__ int of(int len) const { return len > tokens ? (len + tokens - 1) / tokens : 1; }
-    // all tiles, and how many workgroups are worth while: a pair is split where each part has `enough`
+    // workgroups that a pair of n tiles is worth: more than one where each has `enough`
+    __device__ int worth(int n) const { return n < 2 * enough ? 1 : n / enough; }
     __device__ void total(unsigned* tiles, unsigned* groups) const
     {
         const int lane = threadIdx.x & 63;
-        int sum = 0, worth = 0;
+        int sum = 0, all = 0;
         for (int s = lane; s < seqs; s += 64) {
             const int n = of(clamp_length(lengths[s], capacity));
             sum += n;
-            worth += n < 2 * enough ? 1 : n / enough;
+            all += worth(n);
         }
         *tiles = (unsigned)__builtin_amdgcn_readlane(wave_scan(sum), 63) * per_seq;
-        *groups = (unsigned)__builtin_amdgcn_readlane(wave_scan(worth), 63) * per_seq;
+        *groups = (unsigned)__builtin_amdgcn_readlane(wave_scan(all), 63) * per_seq;
     }
-    // the sequence that tile u belongs to, and its first tile
-    __device__ int find(int u, int* first) const
+    // the sequence that tile (by_worth: workgroup) u belongs to, and its first one
+    __device__ int find(int u, bool by_worth, int* first) const
     {
         const int lane = threadIdx.x & 63;
         int before = 0;
         for (int s0 = 0; s0 < seqs; s0 += 64) {
-            const int sum = wave_scan(s0 + lane < seqs ? of(clamp_length(lengths[s0 + lane], capacity)) * per_seq : 0);
+            const int n = s0 + lane < seqs ? of(clamp_length(lengths[s0 + lane], capacity)) : 0;
+            const int sum = wave_scan((by_worth && n ? worth(n) : n) * per_seq);
             const unsigned long long past = __ballot(before + sum > u);
             if (past) {
                 const int at = __builtin_ctzll(past);
@@ -112,26 +116,34 @@ struct Deal {
 // How a type's tiles look.  PE: consecutive values of a row that a lane takes of V, NP such pieces 16 * PE apart.
 template <typename T, int DP> struct Tile;
 template <int DP> struct Tile<uint16_t, DP> {
-    static constexpr int WAVES = DP == 256 ? 4 : 8;
+    static constexpr int WAVES = DP == 256 ? 4 : (DP == 64 ? 16 : 8);
     static constexpr int TOKENS = 32, PE = DP == 64 ? 4 : 8, NP = DP / (16 * PE);
     static constexpr int KSTEPS = DP / 32;       // of S^T: 32 values of a head a step
 };
 template <int DP> struct Tile<float, DP> {
-    static constexpr int WAVES = DP == 256 ? 4 : 8;
+    static constexpr int WAVES = DP == 256 ? 4 : (DP == 64 ? 16 : 8);
     static constexpr int TOKENS = 16, PE = 4, NP = DP / (16 * PE);
     static constexpr int KSTEPS = DP / 16;       // four steps of 4 values
 };
 
 // A wavefront's pages: lane x has that of its sub-tile x (16 tokens) of the next 64.
-template <int SUB> __device__ __forceinline__ int load_pages(const int32_t* table, int shift, int n_pages, int tile, int len)
+template <int SUB> __device__ __forceinline__ int load_pages(const int32_t* table, int shift, int n_pages, int tile, int step, int len)
 {
-    const int tok = (tile * SUB + (int)(threadIdx.x & 63)) * 16;
+    const int lane = threadIdx.x & 63, tok = ((tile + lane / SUB * step) * SUB + lane % SUB) * 16;
     int page = -1;
     if (tok < len) page = table[tok >> shift];
     return (unsigned)page < (unsigned)n_pages ? page : -1;
 }
 
-template <typename V> __device__ __forceinline__ V load_once(const void* p) { return __builtin_nontemporal_load(reinterpret_cast<const V*>(p)); }
+// Rows of a page through a buffer descriptor that ends with the last token: what lies behind it reads as zero, without a branch, and lanes
+// that have no value of a row ask for an offset that is always behind it.  Values are read once: around the caches.
+constexpr int NOWHERE = 0x40000000;
+template <int BYTES> __device__ __forceinline__ auto load_row(__amdgpu_buffer_rsrc_t rows, int offset)
+{
+    constexpr int AROUND = 2;          // non-temporal
+    if constexpr (BYTES == 16) return __builtin_amdgcn_raw_buffer_load_b128(rows, offset, 0, AROUND);
+    else return __builtin_amdgcn_raw_buffer_load_b64(rows, offset, 0, AROUND);
+}
 
 template <typename T, int DP>
 __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const AttendArgs a)
@@ -145,24 +157,41 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
     // a wavefront's two parts: of what begins before its run, and of what goes on behind it
     __shared__ __align__(16) float s_o[2 * WAVES][ROWS][DP + 4];
     __shared__ float s_m[2 * WAVES][ROWS], s_l[2 * WAVES][ROWS];
-    __shared__ int s_first[2 * WAVES];                                 // first tile of the pair that a part belongs to, -1: no part
-    __shared__ int s_seq[2 * WAVES], s_pair[2 * WAVES], s_tiles[2 * WAVES];
+    __shared__ int4 s_part[2 * WAVES];                                 // its pair's first tile (-1: no part), sequence, number, tiles
     __shared__ int s_last[2];
 
     const Cache& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
     const int D = c.dim, per_seq = c.heads * a.blocks;
-    const Tiles tiles{c.lengths, c.seqs, c.capacity, per_seq, TL::TOKENS, a.rounds * WAVES};
+    const Tiles tiles{c.lengths, c.seqs, c.capacity, per_seq, TL::TOKENS, SPLIT_TILES * WAVES};
     unsigned total, groups;
     tiles.total(&total, &groups);
-    groups = groups < gridDim.x ? groups : gridDim.x;
+    const bool own_group = groups <= gridDim.x;                        // of a pair
+    groups = own_group ? groups : gridDim.x;
     if (blockIdx.x >= groups) return;
     const Deal deal(total, groups);
-    const int run = deal.first(blockIdx.x);
-    const Deal own(deal.first(blockIdx.x + 1) - run, WAVES);
+    // this workgroup's run of tiles (with groups of their own counted from the sequence's first), the sequence that it begins in and that one's first tile
+    int run, run_end, seq, first = 0, part = 0, parts = 1;
+    if (own_group) {
+        int first_group;
+        seq = tiles.find(blockIdx.x, true, &first_group);
+        if (seq >= c.seqs) return;
+        const int n = tiles.of(clamp_length(c.lengths[seq], c.capacity));
+        parts = tiles.worth(n);
+        const int at = (int)blockIdx.x - first_group, pair = (unsigned)at / (unsigned)parts;
+        part = at - pair * parts;
+        const Deal split(n, parts);
+        run = pair * n + split.first(part);
+        run_end = pair * n + split.first(part + 1);
+    } else {
+        run = deal.first(blockIdx.x);
+        run_end = deal.first(blockIdx.x + 1);
+    }
+    const Deal own(run_end - run, WAVES);
     int u = run + own.first(wave);
-    const int end = run + own.first(wave + 1);
-    if (lane < 2) s_first[2 * wave + lane] = -1;
+    int end = run + own.first(wave + 1);
+    int step = 1;
+    if (lane < 2) s_part[2 * wave + lane].x = -1;
 
     // A run is worked through a pair (sequence, head, block) at a time: those of its tiles that fall into one.
     struct Stretch {
@@ -186,74 +215,45 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
     struct Where { long at[SUB]; int left[SUB]; };
     key_t q[KSTEPS], k[SUB][KSTEPS];
     piece_t v[SUB][4][NP];
-    int t = 0, t1 = 0, pages = -1, ahead = -1, used = 0;       // tiles t .. t1 - 1, their pages
-    Where here, next;
-    auto find = [&](const Stretch& x, int tile, int slot) {
+    int pages = -1, ahead = -1, used = 0;                      // of the tiles that come
+    auto find = [&](const Stretch& x, int tile) {
         Where w;
 #pragma unroll
         for (int s = 0; s < SUB; ++s) {
-            const int tok = tile * TL::TOKENS + 16 * s, page = __builtin_amdgcn_readlane(pages, slot * SUB + s);
+            const int tok = tile * TL::TOKENS + 16 * s, page = __builtin_amdgcn_readlane(pages, used * SUB + s);
             w.left[s] = page >= 0 ? (x.len - tok < 16 ? x.len - tok : 16) : 0;
             w.at[s] = page >= 0 ? ((((long)page * c.heads + x.h) << c.page_shift) + (tok & ((1 << c.page_shift) - 1))) * D : 0;
         }
         return w;
     };
-    auto full = [&](const Where& w) {
-        bool f = D == DP;
-#pragma unroll
-        for (int s = 0; s < SUB; ++s) f = f && w.left[s] == 16;
-        return f;
+    auto rows_of = [&](const void* pages, const Where& w, int s) {
+        return __builtin_amdgcn_make_buffer_rsrc((char*)pages + w.at[s] * (long)sizeof(T), 0, w.left[s] * D * (int)sizeof(T), 0x00027000);
     };
     auto load_k = [&](const Where& w) {
-        const bool all = full(w);
 #pragma unroll
         for (int s = 0; s < SUB; ++s) {
-            const T* src = (const T*)c.k + w.at[s] + l16 * D;
-            if (all) {
+            const __amdgpu_buffer_rsrc_t rows = rows_of(c.k, w, s);
 #pragma unroll
-                for (int i = 0; i < KSTEPS; ++i) k[s][i] = load_once<key_t>(src + (4 * i + quad) * (16 / (int)sizeof(T)));
-            } else {
-#pragma unroll
-                for (int i = 0; i < KSTEPS; ++i) {
-                    const int d = (4 * i + quad) * (16 / (int)sizeof(T));
-                    k[s][i] = key_t(0);
-                    if (l16 < w.left[s] && d < D) k[s][i] = load_once<key_t>(src + d);
-                }
+            for (int i = 0; i < KSTEPS; ++i) {
+                const int d = (4 * i + quad) * (16 / (int)sizeof(T));
+                k[s][i] = load_row<16>(rows, d < D ? (l16 * D + d) * (int)sizeof(T) : NOWHERE);
             }
         }
     };
     auto load_v = [&](const Where& w) {
-        const bool all = full(w);
 #pragma unroll
         for (int s = 0; s < SUB; ++s) {
-            const T* src = (const T*)c.v + w.at[s] + 4 * quad * D;
-            if (all) {
+            const __amdgpu_buffer_rsrc_t rows = rows_of(c.v, w, s);
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-                    for (int p = 0; p < NP; ++p) v[s][r][p] = load_once<piece_t>(src + r * D + (16 * p + l16) * PE);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int p = 0; p < NP; ++p) {
-                        const int d = (16 * p + l16) * PE;
-                        v[s][r][p] = piece_t(0);
-                        if (4 * quad + r < w.left[s] && d < D) v[s][r][p] = load_once<piece_t>(src + r * D + d);
-                    }
-            }
+                for (int p = 0; p < NP; ++p) {
+                    const int d = (16 * p + l16) * PE;
+                    v[s][r][p] = load_row<PE * (int)sizeof(T)>(rows, d < D ? ((4 * quad + r) * D + d) * (int)sizeof(T) : NOWHERE);
+                }
         }
     };
-    // what a stretch begins with: its pages, query heads, and first tile
-    auto begin = [&](const Stretch& x) {
-        const int32_t* table = c.table + (long)x.seq * c.max_pages;
-        t = x.from;
-        t1 = x.len > 0 ? x.to : t;
-        used = 0;
-        pages = load_pages<SUB>(table, c.page_shift, c.n_pages, t, x.len);
-        ahead = -1;
-        if (t + 64 / SUB < t1) ahead = load_pages<SUB>(table, c.page_shift, c.n_pages, t + 64 / SUB, x.len);
-        // this lane's part of the query heads: head l16, values 32 * i + 8 * quad .. (or 16 * i + 4 * quad ..)
+    auto load_q = [&](const Stretch& x) {                      // head l16, values 32 * i + 8 * quad .. (or 16 * i + 4 * quad ..)
         const T* src = (const T*)a.j.q.data + (long)x.seq * a.j.q.token + (long)(x.h * a.group + x.row0 + l16) * a.j.q.head;
         constexpr int E = 16 / (int)sizeof(T);
 #pragma unroll
@@ -270,24 +270,21 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                 }
             }
         }
-        if (t < t1) {
-            here = find(x, t, 0);
-            load_k(here);
-            load_v(here);
-        }
     };
 
     // row, values d and d + 1 of a pair's result: x and y over L
+    auto store_pair = [&](int seq, int head, int d, float x, float y) {
+        if (d >= D) return;
+        T* out = (T*)a.j.out.data + (long)seq * a.j.out.token + (long)head * a.j.out.head + d;
+        T e0, e1;
+        narrow(x, e0);
+        narrow(y, e1);
+        out[0] = e0;
+        out[1] = e1;
+    };
     auto finish = [&](int seq, int head, int d, float M, float L, float x, float y) {
         const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-        if (d < D) {
-            T* out = (T*)a.j.out.data + (long)seq * a.j.out.token + (long)head * a.j.out.head + d;
-            T e0, e1;
-            narrow(x * inv, e0);
-            narrow(y * inv, e1);
-            out[0] = e0;
-            out[1] = e1;
-        }
+        store_pair(seq, head, d, x * inv, y * inv);
         if (d == 0) {
             const float z = L == 0.0f ? -__builtin_inff() : M + __builtin_amdgcn_logf(L) * LN2;
             if (a.j.lse) a.j.lse[(long)seq * a.j.q.heads + head] = z;
@@ -295,25 +292,32 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
         }
     };
 
-    Stretch x;
-    bool over = true;
-    if (u < end) {
-        int first;
-        const int seq = tiles.find(u, &first);
-        if (seq < c.seqs) {
-            over = false;
-            x = stretch(seq, first);
-            begin(x);
-        }
-    }
-    while (!over) {
-        float m = LOWEST, l = 0.0f;
-        f32x4 o[NP * PE];
+    // The tiles in order, those of the run's pairs behind each other: while one is computed the next one comes, its keys while this one's
+    // weights are made, its values while the next one's scores are.
+    Stretch x, y;                                              // of this tile, of the next one
+    int t = 0, ty = 0;                                         // the tiles
+    bool here = false, more = u < end;                         // there is one
+    Where w, wy;
+    float m = LOWEST, l = 0.0f;
+    f32x4 o[NP * PE];
 #pragma unroll
-        for (int i = 0; i < NP * PE; ++i) o[i] = f32x4{0, 0, 0, 0};
-        for (; t < t1; ++t) {
+    for (int i = 0; i < NP * PE; ++i) o[i] = f32x4{0, 0, 0, 0};
+    if (more) {
+        if (!own_group) seq = tiles.find(u, false, &first);
+        // a run within one pair: the wavefronts take its tiles in turn, so that they read one stretch of memory together
+        const int n = seq < c.seqs ? tiles.of(clamp_length(c.lengths[seq], c.capacity)) : 1;
+        if (run_end - run >= WAVES && run >= first && (unsigned)(run - first) / (unsigned)n == (unsigned)(run_end - 1 - first) / (unsigned)n) {
+            step = WAVES;
+            u = run;
+            end = run_end;
+        }
+        more = seq < c.seqs;
+    }
+    bool fresh = true;                                         // the next tile begins a stretch
+    for (;;) {
+        f32x4 sc[SUB];
+        if (here) {
             // scores of tokens 16 * s + 4 * quad + r for query head l16
-            f32x4 sc[SUB];
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
                 sc[s] = f32x4{0, 0, 0, 0};
@@ -322,23 +326,31 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                     if constexpr (HALF)
                         sc[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[s][i]), __builtin_bit_cast(bf16x8, q[i]), sc[s], 0, 0, 0);
                     else {
-                        const f32x4 x = __builtin_bit_cast(f32x4, k[s][i]), y = __builtin_bit_cast(f32x4, q[i]);
+                        const f32x4 ka = __builtin_bit_cast(f32x4, k[s][i]), qa = __builtin_bit_cast(f32x4, q[i]);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) sc[s] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], sc[s], 0, 0, 0);
+                        for (int e = 0; e < 4; ++e) sc[s] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[e], qa[e], sc[s], 0, 0, 0);
                     }
                 }
             }
-            // the next tile's keys come while this one's weights are made, its values while the next one's scores are
-            const bool more = t + 1 < t1;
-            if (more) {
-                if (++used == 64 / SUB) {
-                    used = 0;
-                    pages = ahead;
-                    if (t + 1 + 64 / SUB < t1) ahead = load_pages<SUB>(c.table + (long)x.seq * c.max_pages, c.page_shift, c.n_pages, t + 1 + 64 / SUB, x.len);
-                }
-                next = find(x, t + 1, used);
-                load_k(next);
+        }
+        // the next tile: of this stretch, or the first one of the next
+        if (more) {
+            if (fresh) {
+                y = stretch(seq, first);
+                ty = y.from + (step > 1 ? wave : 0);
+                used = 0;
+                pages = load_pages<SUB>(c.table + (long)y.seq * c.max_pages, c.page_shift, c.n_pages, ty, step, y.len);
+                load_q(y);
+            } else if (++used == 64 / SUB) {
+                used = 0;
+                pages = ahead;
             }
+            if (used == 0 && ty + 64 / SUB * step < y.to)
+                ahead = load_pages<SUB>(c.table + (long)y.seq * c.max_pages, c.page_shift, c.n_pages, ty + 64 / SUB * step, step, y.len);
+            wy = find(y, ty);
+            load_k(wy);
+        }
+        if (here) {
             float top = LOWEST;
 #pragma unroll
             for (int s = 0; s < SUB; ++s)
@@ -346,7 +358,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                 for (int r = 0; r < 4; ++r) {
                     float y = sc[s][r] * a.j.scale;
                     if (a.j.softcap > 0.0f) y = a.j.softcap * tanhf(y / a.j.softcap);
-                    y = 4 * quad + r < here.left[s] ? y : -__builtin_inff();
+                    y = 4 * quad + r < w.left[s] ? y : -__builtin_inff();
                     sc[s][r] = y;
                     top = fmaxf(top, y);
                 }
@@ -406,128 +418,143 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                         for (int r = 0; r < 4; ++r)
                             o[pc * PE + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[0][r][pc][e]), p[0][r], o[pc * PE + e], 0, 0, 0);
             }
-            if (more) {
-                load_v(next);
-                here = next;
-            }
         }
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-
-        // the next stretch begins to come while this one is put away
-        const Stretch done = x;
-        u += done.to - done.from;
-        const bool same = u - done.first < done.n * per_seq;
-        const int seq = same ? done.seq : done.seq + 1;
-        over = u >= end || seq >= c.seqs;
-        if (!over) {
-            x = stretch(seq, same ? done.first : done.first + done.n * per_seq);
-            begin(x);
-        }
-        // lane has o of query head l16, values (16 * p + 4 * quad + r) * PE + e: runs of 4 * PE values
-        if (done.from == 0 && done.to == done.n) {
-            const int head = done.h * a.group + done.row0 + l16;
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            if (l16 < done.rows) {
-                T* out = (T*)a.j.out.data + (long)done.seq * a.j.out.token + (long)head * a.j.out.head;
-                constexpr int E = 16 / (int)sizeof(T);
+        if (more) load_v(wy);
+        if (here && t + step >= x.to) {
+            // the pair is through, as far as this wavefront has to do with it
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            // lane has o of query head l16, values (16 * p + 4 * quad + r) * PE + e: runs of 4 * PE values
+            if (x.from == 0 && x.to == x.n && step == 1) {
+                const int head = x.h * a.group + x.row0 + l16;
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                if (l16 < x.rows) {
+                    T* out = (T*)a.j.out.data + (long)x.seq * a.j.out.token + (long)head * a.j.out.head;
+                    constexpr int E = 16 / (int)sizeof(T);
 #pragma unroll
-                for (int p = 0; p < NP; ++p)
+                    for (int p = 0; p < NP; ++p)
 #pragma unroll
-                    for (int y = 0; y < 4 * PE / E; ++y) {
-                        const int d = (16 * p + 4 * quad) * PE + y * E;
-                        T w[E];
+                        for (int i = 0; i < 4 * PE / E; ++i) {
+                            const int d = (16 * p + 4 * quad) * PE + i * E;
+                            T e[E];
 #pragma unroll
-                        for (int z = 0; z < E; ++z) narrow(o[p * PE + (y * E + z) % PE][(y * E + z) / PE] * inv, w[z]);
-                        if (d < D) {
-                            if (a.out_aligned) {
-                                key_t word;
-                                __builtin_memcpy(&word, w, 16);
-                                *reinterpret_cast<key_t*>(out + d) = word;
-                            } else
+                            for (int z = 0; z < E; ++z) narrow(o[p * PE + (i * E + z) % PE][(i * E + z) / PE] * inv, e[z]);
+                            if (d < D) {
+                                if (a.out_aligned) {
+                                    key_t word;
+                                    __builtin_memcpy(&word, e, 16);
+                                    *reinterpret_cast<key_t*>(out + d) = word;
+                                } else
 #pragma unroll
-                                for (int z = 0; z < E; ++z) out[d + z] = w[z];
+                                    for (int z = 0; z < E; ++z) out[d + z] = e[z];
+                            }
                         }
+                    if (quad == 0) {
+                        const float z = l == 0.0f ? -__builtin_inff() : m + __builtin_amdgcn_logf(l) * LN2;
+                        if (a.j.lse) a.j.lse[(long)x.seq * a.j.q.heads + head] = z;
+                        a.lse[(long)x.seq * a.j.q.heads + head] = z;
                     }
-                if (quad == 0) {
-                    const float z = l == 0.0f ? -__builtin_inff() : m + __builtin_amdgcn_logf(l) * LN2;
-                    if (a.j.lse) a.j.lse[(long)done.seq * a.j.q.heads + head] = z;
-                    a.lse[(long)done.seq * a.j.q.heads + head] = z;
                 }
-            }
-        } else {
-            const int slot = 2 * wave + (done.from == 0 ? 1 : 0);
-            if (quad == 0) { s_m[slot][l16] = m; s_l[slot][l16] = l; }
-            if (l16 < done.rows) {
+            } else {
+                const int slot = 2 * wave + (x.from == 0 && (step == 1 || wave == 0) ? 1 : 0);
+                if (quad == 0) { s_m[slot][l16] = m; s_l[slot][l16] = l; }
+                if (l16 < x.rows) {
 #pragma unroll
-                for (int p = 0; p < NP; ++p)
+                    for (int p = 0; p < NP; ++p)
 #pragma unroll
-                    for (int y = 0; y < PE; ++y) {
-                        f32x4 w;
+                        for (int i = 0; i < PE; ++i) {
+                            f32x4 e;
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) w[z] = o[p * PE + (4 * y + z) % PE][(4 * y + z) / PE];
-                        *reinterpret_cast<f32x4*>(&s_o[slot][l16][(16 * p + 4 * quad) * PE + 4 * y]) = w;
-                    }
+                            for (int z = 0; z < 4; ++z) e[z] = o[p * PE + (4 * i + z) % PE][(4 * i + z) / PE];
+                            *reinterpret_cast<f32x4*>(&s_o[slot][l16][(16 * p + 4 * quad) * PE + 4 * i]) = e;
+                        }
+                }
+                if (lane == 0) s_part[slot] = make_int4(x.first + x.pair * x.n, x.seq, x.pair, x.n);
             }
-            if (lane == 0) {
-                s_first[slot] = done.first + done.pair * done.n;
-                s_seq[slot] = done.seq;
-                s_pair[slot] = done.pair;
-                s_tiles[slot] = done.n;
-            }
+            m = LOWEST;
+            l = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NP * PE; ++i) o[i] = f32x4{0, 0, 0, 0};
+        }
+        here = more;
+        if (!here) break;
+        if (fresh) x = y;
+        t = ty;
+        w = wy;
+        // and what comes behind that one
+        ty += step;
+        fresh = ty >= y.to;
+        if (fresh) {
+            u += y.to - y.from;
+            if (u - y.first >= y.n * per_seq) { ++seq; first += y.n * per_seq; }
+            more = u < end && seq < c.seqs;
         }
     }
     __syncthreads();
 
     // The parts of a pair: the first one a part that goes on behind its wavefront's run (or the workgroup's first part, of what begins before its
     // run), the others the first parts of the wavefronts behind.  Wavefronts without tiles are behind all others.
-    struct Chain { int slot, wave, parts, seq, first, n, pair, head0, rows; };
+    const int4 of_slot = s_part[lane & (2 * WAVES - 1)];       // a slot a lane
+    struct Chain { int slot, wave, parts, seq, first, n, head0, rows; };
     auto chain = [&](int slot) {
         Chain x;
         x.slot = slot;
-        x.first = __builtin_amdgcn_readfirstlane(s_first[slot]);
-        x.seq = __builtin_amdgcn_readfirstlane(s_seq[slot]);
-        x.pair = __builtin_amdgcn_readfirstlane(s_pair[slot]);
-        x.n = __builtin_amdgcn_readfirstlane(s_tiles[slot]);
+        x.first = __builtin_amdgcn_readlane(of_slot.x, slot);
+        x.seq = __builtin_amdgcn_readlane(of_slot.y, slot);
+        const int pair = __builtin_amdgcn_readlane(of_slot.z, slot);
+        x.n = __builtin_amdgcn_readlane(of_slot.w, slot);
         x.wave = slot >> 1;
-        x.parts = 1;
-        while (x.wave + x.parts < WAVES && __builtin_amdgcn_readfirstlane(s_first[2 * (x.wave + x.parts)]) == x.first) ++x.parts;
-        const int h = (unsigned)x.pair / (unsigned)a.blocks, row0 = (x.pair - h * a.blocks) * ROWS;
+        // the run of wavefronts behind whose first parts are of the same pair
+        const unsigned long long others = ~__ballot((lane & 1) == 0 && lane < 2 * WAVES && of_slot.x == x.first) & 0x5555555555555555ull;
+        x.parts = (__builtin_ctzll(others >> (2 * x.wave + 2) | 1ull << (2 * (WAVES - 1 - x.wave))) >> 1) + 1;
+        const int h = (unsigned)pair / (unsigned)a.blocks, row0 = (pair - h * a.blocks) * ROWS;
         x.head0 = h * a.group + row0;
         x.rows = a.group - row0 < ROWS ? a.group - row0 : ROWS;
         return x;
     };
-    // slots s0, s0 + step, ... of row, values d and d + 1
+    // slot s0 and the first slots of the wavefronts behind `rest`, `parts` in all: row, values d and d + 1
     auto join = [&](int s0, int rest, int parts, int row, int d, float* M, float* L, float* x, float* y) {
-        *M = s_m[s0][row];
-        for (int p = 1; p < parts; ++p) *M = fmaxf(*M, s_m[rest + 2 * p][row]);
+        float mp[WAVES], lp[WAVES];
+        float2 v[WAVES];
+        *M = LOWEST;
+#pragma unroll
+        for (int p = 0; p < WAVES; ++p) {
+            mp[p] = LOWEST;
+            lp[p] = 0.0f;
+            v[p] = make_float2(0.0f, 0.0f);
+            if (p < parts) {
+                const int s = p == 0 ? s0 : 2 * (rest + p);
+                mp[p] = s_m[s][row];
+                lp[p] = s_l[s][row];
+                v[p] = *reinterpret_cast<const float2*>(&s_o[s][row][d]);
+            }
+            *M = fmaxf(*M, mp[p]);
+        }
         *L = *x = *y = 0.0f;
-        for (int p = 0; p < parts; ++p) {
-            const int s = p == 0 ? s0 : rest + 2 * p;
-            const float f = exp_of(s_m[s][row] - *M);
-            const float2 v = *reinterpret_cast<const float2*>(&s_o[s][row][d]);
-            *L += f * s_l[s][row];
-            *x += f * v.x;
-            *y += f * v.y;
+#pragma unroll
+        for (int p = 0; p < WAVES; ++p) {
+            const float f = exp_of(mp[p] - *M);
+            *L += f * lp[p];
+            *x += f * v[p].x;
+            *y += f * v[p].y;
         }
     };
     bool mine[2] = {false, false};                             // parts of this workgroup that others have to do with
-    const int run_end = deal.first(blockIdx.x + 1);
-    for (int slot = 0; slot < 2 * WAVES; ++slot) {
-        // a part that begins before its wavefront's run belongs to the chain of an earlier one, but for the workgroup's first
-        if ((slot > 0 && (slot & 1) == 0) || s_first[slot] < 0) continue;
-        const Chain x = chain(slot);
+    // (a part that begins before its wavefront's run belongs to the chain of an earlier one, but for the workgroup's first)
+    const unsigned long long heads = __ballot(lane < 2 * WAVES && of_slot.x >= 0 && (lane == 0 || (lane & 1)));
+    for (unsigned long long rest = heads; rest; rest &= rest - 1) {
+        const Chain x = chain(__builtin_ctzll(rest));
         const bool whole = x.first >= run && x.first + x.n <= run_end;
         const int w = x.first < run ? 0 : 1;
-        float* part = a.parts + (2L * blockIdx.x + w) * part_floats<DP>();
+        float* to = a.parts + (2L * blockIdx.x + w) * part_floats<DP>();
         for (int i = 2 * tid; i < x.rows * DP; i += 2 * THREADS) {
             const int row = i / DP, d = i % DP;
             float M, L, y, z;
-            join(x.slot, 2 * x.wave, x.parts, row, d, &M, &L, &y, &z);
+            join(x.slot, x.wave, x.parts, row, d, &M, &L, &y, &z);
             if (whole) finish(x.seq, x.head0 + row, d, M, L, y, z);
             else {
-                put(part + 2 * ROWS + i, y, z);
-                if (d == 0) put(part + 2 * row, M, L);
+                put(to + 2 * ROWS + i, y, z);
+                if (d == 0) put(to + 2 * row, M, L);
             }
         }
         if (!whole) mine[w] = true;
@@ -540,14 +567,10 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
     unsigned w0[2] = {0, 0}, w1[2] = {0, 0};
     for (int w = 0; w < 2; ++w)
         if (mine[w]) {
-            int slot = 0;                        // the workgroup's first part, or the last one that goes on
-            if (w == 1)
-                for (int y = 0; y < WAVES; ++y)
-                    if (s_first[2 * y + 1] >= 0) slot = 2 * y + 1;
-            slots[w] = slot;
-            const unsigned u0 = __builtin_amdgcn_readfirstlane(s_first[slot]);
-            w0[w] = deal.owner(u0);
-            w1[w] = deal.owner(u0 + __builtin_amdgcn_readfirstlane(s_tiles[slot]) - 1);
+            slots[w] = w == 0 ? 0 : 63 - __builtin_clzll(heads);       // the workgroup's first part, or the last one that goes on
+            const unsigned u0 = __builtin_amdgcn_readlane(of_slot.x, slots[w]);
+            w0[w] = own_group ? blockIdx.x - part : deal.owner(u0);
+            w1[w] = own_group ? w0[w] + parts - 1 : deal.owner(u0 + __builtin_amdgcn_readlane(of_slot.w, slots[w]) - 1);
             if (tid == w) {
                 int* counter = a.counters + w0[w];
                 s_last[w] = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)(w1[w] - w0[w]);
@@ -559,52 +582,71 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
         if (!mine[w] || !s_last[w]) continue;
         const Chain x = chain(slots[w]);
         const int rows = x.rows;
-        __syncthreads();                         // (everyone has read what the parts are of)
-        // Each wavefront takes every WAVES-th part, in order; then the wavefronts are joined.  A part is a trip to memory past
-        // the caches: four parts of four values a lane are on their way at once.
-        for (int i0 = 2 * lane; i0 < rows * DP; i0 += 512) {
-            float M[4], L[4], y[4], z[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) { M[k] = LOWEST; L[k] = y[k] = z[k] = 0.0f; }
-            for (unsigned g0 = w0[w] + wave; g0 <= w1[w]; g0 += 4 * WAVES) {
-                float2 ml[4][4], xy[4][4];
-#pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const unsigned g = g0 + n * WAVES;
-                    const float* part = a.parts + (2L * g + (g == w0[w] ? 1 : 0)) * part_floats<DP>();
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int i = i0 + 128 * k;
-                        ml[n][k] = make_float2(LOWEST, 0.0f);
-                        xy[n][k] = make_float2(0.0f, 0.0f);
-                        if (g <= w1[w] && i < rows * DP) { ml[n][k] = get(part + 2 * (i / DP)); xy[n][k] = get(part + 2 * ROWS + i); }
-                    }
-                }
-#pragma unroll
-                for (int n = 0; n < 4; ++n)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float top = fmaxf(M[k], ml[n][k].x), f = exp_of(M[k] - top), g = exp_of(ml[n][k].x - top);
-                        M[k] = top;
-                        L[k] = f * L[k] + g * ml[n][k].y;
-                        y[k] = f * y[k] + g * xy[n][k].x;
-                        z[k] = f * z[k] + g * xy[n][k].y;
-                    }
+        // the weight of every part, a query head a wavefront at a time (LDS is free but for what the parts are of, which is in registers)
+        const int count = (int)(w1[w] - w0[w]) + 1;
+        float* s_weight = &s_o[0][0][0];                       // rows x parts
+        float* s_sum = &s_o[WAVES][0][0];
+        static_assert(WAVES * ROWS * (DP + 4) >= ROWS * MAX_GROUPS, "room for the weights of all parts");
+        auto part_of = [&](int p) { return a.parts + (2L * (w0[w] + p) + (p == 0 ? 1 : 0)) * part_floats<DP>(); };
+#pragma unroll 1
+        for (int row = wave; row < rows; row += WAVES) {
+            float M = LOWEST, L = 0.0f;
+#pragma unroll 1
+            for (int p = lane; p < count; p += 64) {
+                const float2 ml = get(part_of(p) + 2 * row);
+                s_weight[row * count + p] = ml.x;
+                s_sum[row * count + p] = ml.y;
+                M = fmaxf(M, ml.x);
             }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int i = i0 + 128 * k, row = i / DP, d = i % DP;
-                if (i < rows * DP) {
-                    *reinterpret_cast<float2*>(&s_o[2 * wave][row][d]) = make_float2(y[k], z[k]);
-                    if (d == 0) { s_m[2 * wave][row] = M[k]; s_l[2 * wave][row] = L[k]; }
-                }
+            M = wave_max(M);
+#pragma unroll 1
+            for (int p = lane; p < count; p += 64) L += exp_of(s_weight[row * count + p] - M) * s_sum[row * count + p];
+            L = wave_sum(L);
+            const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+#pragma unroll 1
+            for (int p = lane; p < count; p += 64) s_weight[row * count + p] = exp_of(s_weight[row * count + p] - M) * inv;
+            if (lane == 0) {
+                const float z = L == 0.0f ? -__builtin_inff() : M + __builtin_amdgcn_logf(L) * LN2;
+                const long at = (long)x.seq * a.j.q.heads + x.head0 + row;
+                if (a.j.lse) a.j.lse[at] = z;
+                a.lse[at] = z;
             }
         }
         __syncthreads();
-        for (int i = 2 * tid; i < rows * DP; i += 2 * THREADS) {
-            float M, L, y, z;
-            join(0, 0, WAVES, i / DP, i % DP, &M, &L, &y, &z);
-            finish(x.seq, x.head0 + i / DP, i % DP, M, L, y, z);
+        // the sum over the parts, two values a thread: a team of threads for all of them takes every teams-th part, in order
+        const int pairs = rows * DP / 2, teams = THREADS / pairs > 1 ? THREADS / pairs : 1, team = tid / pairs;
+#pragma unroll 1
+        for (int i = teams > 1 ? tid - team * pairs : tid; i < pairs && team < (teams > 1 ? teams : WAVES * 64); i += teams > 1 ? pairs : THREADS) {
+            const int row = 2 * i / DP, d = 2 * i % DP;
+            float y = 0.0f, z = 0.0f;
+#pragma unroll 1
+            for (int p = teams > 1 ? team : 0; p < count; p += 8 * teams) {
+                float2 v[8];
+#pragma unroll
+                for (int n = 0; n < 8; ++n) v[n] = get(part_of(p + n * teams < count ? p + n * teams : p) + 2 * ROWS + 2 * i);
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+                    if (p + n * teams < count) {
+                        const float f = s_weight[row * count + p + n * teams];
+                        y += f * v[n].x;
+                        z += f * v[n].y;
+                    }
+            }
+            if (teams > 1) *reinterpret_cast<float2*>(s_sum + 2 * (team * pairs + i)) = make_float2(y, z);
+            else store_pair(x.seq, x.head0 + row, d, y, z);
+        }
+        if (teams > 1) {
+            __syncthreads();
+            if (team == 0) {
+                float y = 0.0f, z = 0.0f;
+#pragma unroll 1
+                for (int n = 0; n < teams; ++n) {
+                    const float2 v = *reinterpret_cast<const float2*>(s_sum + 2 * (n * pairs + tid));
+                    y += v.x;
+                    z += v.y;
+                }
+                store_pair(x.seq, x.head0 + 2 * tid / DP, 2 * tid % DP, y, z);
+            }
         }
         __syncthreads();
     }
@@ -656,7 +698,6 @@ hipError_t launch_attend(const AttendJob& j, const Cache& c, hipStream_t st)
     a.pitch = c.capacity;
     const int dp = c.dim <= 64 ? 64 : (c.dim <= 128 ? 128 : 256);
     a.out_aligned = (uintptr_t)j.out.data % 16 == 0 && j.out.token % align == 0 && j.out.head % align == 0;
-    const char* E = getenv("CB_R"); a.rounds = E ? atoi(E) : 2;
     // one workgroup a compute unit, no more than there can be tiles
     const long most = (long)c.seqs * c.heads * a.blocks * (c.capacity / (c.bf16 ? 32 : 16) + 1);
     const long want = device_units();

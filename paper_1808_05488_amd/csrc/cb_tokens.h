@@ -110,6 +110,24 @@ __device__ __forceinline__ int wave_max(int v)
     return __builtin_amdgcn_readlane(v, 63);
 }
 __device__ __forceinline__ uint32_t wave_max_unsigned(uint32_t v) { return (uint32_t)wave_max((int)(v ^ 0x80000000u)) ^ 0x80000000u; }
+// The sum of all lanes, in a fixed order, in every lane.
+__device__ __forceinline__ float wave_sum(float v)
+{
+    auto add = [](float a, int b) { return a + __uint_as_float((uint32_t)b); };
+    v = add(v, __builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x111, 0xf, 0xf, false));
+    v = add(v, __builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x112, 0xf, 0xf, false));
+    v = add(v, __builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x114, 0xf, 0xf, false));
+    v = add(v, __builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x118, 0xf, 0xf, false));
+    v = add(v, __builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x142, 0xa, 0xf, false));
+    v = add(v, __builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x143, 0xc, 0xf, false));
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+}
+// The largest of all lanes, none of which is not a number, in every lane.
+__device__ __forceinline__ float wave_max(float v)
+{
+    const uint32_t b = __float_as_uint(v), m = wave_max_unsigned(b & 0x80000000u ? ~b : b | 0x80000000u);
+    return __uint_as_float(m & 0x80000000u ? m & 0x7FFFFFFFu : ~m);
+}
 // Length of a sequence, whatever the array holds.
 __device__ __forceinline__ int clamp_length(int n, int capacity) { return n < 0 ? 0 : (n > capacity ? capacity : n); }
 #endif
