@@ -443,6 +443,13 @@ class Layer:
         idx = _raw_to_host(idx_p, n, self.device)
         return m_t, mt_t, idx.astype(np.int32), n
 
+    def listed(self):
+        """(list, count) of the last frame's changed output pixels as views of the layer's own memory: Ho * Wo int32 linear indices, of which the
+        first count[0] are the last frame's, in ascending order.  Nothing waits; the next frame overwrites both."""
+        idx, cnt = C.c_void_p(), C.c_void_p()
+        _check(lib().cb_layer_changes(self.handle, None, None, C.byref(idx), C.byref(cnt)), "cb_layer_changes")
+        return (_view(self.state_buf, idx.value, (self.Ho * self.Wo,), torch.int32), _view(self.state_buf, cnt.value, (1,), torch.int32))
+
     def state(self) -> torch.Tensor:
         return self._views(cb_layer_state(self.handle), (self.C, self.H, self.W))
 
@@ -624,6 +631,12 @@ def _heads(t: torch.Tensor, what: str, dtype, index: int, dim: int, heads: Optio
     return _pack_heads(t.data_ptr(), stride[0], stride[1], shape[1], 0)
 
 
+def _fresh(t: torch.Tensor, dim: int) -> bytes:
+    """... of a dense one that was made for the call."""
+    heads = t.shape[1]
+    return _pack_heads(t.data_ptr(), heads * dim, dim, heads, 0)
+
+
 def _dense(t: Optional[torch.Tensor], what: str, dtype, index: int, shape) -> Optional[int]:
     """Address of a dense array of that type and shape (None: not given)."""
     if t is None:
@@ -654,14 +667,19 @@ class Rotary:
         inverse: turned back, which is also the gradient of q from that of q_out.  An output may be its input."""
         n, dtype, index, dim = q.shape[0], q.dtype, q.get_device(), self.head_dim
         assert index >= 0 and dtype in _CB_DT, f"q: {dtype} on {q.device}"
+        a, c, d = _heads(q, "q", dtype, index, dim), None, None
         if q_out is None:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        a, b = _heads(q, "q", dtype, index, dim), _heads(q_out, "q_out", dtype, index, dim, q.shape[1], n)
-        c = d = None
+            b = _fresh(q_out, dim)
+        else:
+            b = _heads(q_out, "q_out", dtype, index, dim, q.shape[1], n)
         if k is not None:
+            c = _heads(k, "k", dtype, index, dim, None, n)
             if k_out is None:
                 k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
-            c, d = _heads(k, "k", dtype, index, dim, None, n), _heads(k_out, "k_out", dtype, index, dim, k.shape[1], n)
+                d = _fresh(k_out, dim)
+            else:
+                d = _heads(k_out, "k_out", dtype, index, dim, k.shape[1], n)
         status = lib().cb_rotate(self._address, _CB_DT[dtype], n, _dense(positions, "positions", torch.int32, index, (n, self.n_axes)),
                                  a, b, c, d, 1 if inverse else 0, _raw_stream(index))
         if status:
@@ -739,9 +757,12 @@ class TokenCache:
         b = _heads(v, "v", dtype, i, dim, self.n_kv_heads, n)
         c = d = None
         if q is not None:
+            c = _heads(q, "q", dtype, i, dim, None, n)
             if q_out is None:
                 q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-            c, d = _heads(q, "q", dtype, i, dim, None, n), _heads(q_out, "q_out", dtype, i, dim, q.shape[1], n)
+                d = _fresh(q_out, dim)
+            else:
+                d = _heads(q_out, "q_out", dtype, i, dim, q.shape[1], n)
         status = lib().cb_cache_append(
             self._address, None if rotary is None else rotary._address, n,
             _dense(positions, "positions", torch.int32, i, (n, 1 if rotary is None else rotary.n_axes)),
@@ -762,14 +783,18 @@ class TokenCache:
             self._scratch(heads)
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            b = _fresh(out, dim)
+        else:
+            b = _heads(out, "out", dtype, i, dim, heads, self.n_seq)
         if lse is None:
             like = self._lse.get(heads)
             if like is None:
                 like = self._lse[heads] = torch.empty((self.n_seq, heads), dtype=torch.float32, device=self.device)
             lse = torch.empty_like(like)
-        b = _heads(out, "out", dtype, i, dim, heads, self.n_seq)
+        else:
+            _dense(lse, "lse", torch.float32, i, (self.n_seq, heads))
         status = lib().cb_cache_attend(self._address, _pack_attend(dim ** -0.5 if scale is None else scale, softcap, decay, 1 if accumulate else 0, 0),
-                                       a, b, _dense(lse, "lse", torch.float32, i, (self.n_seq, heads)), _raw_stream(i))
+                                       a, b, lse.data_ptr(), _raw_stream(i))
         if status:
             _check(status, "cb_cache_attend")
         return out, lse

@@ -95,7 +95,7 @@ __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
     // receives them: of free slots too, which the moves write over.
     const bool in_lds = ALL_IN_LDS || len <= a.room;
     int newest = INT32_MIN;
-    i32x4 t[ROUNDS];
+    i32x4 t0 = {0, 0, 0, 0};                                   // times of a thread's first four slots
     // (both as read: then as the ranks want them)
     auto take_over = [&](int i, i32x4& t, f32x4& w) {
         if (a.copies && i < budget) {
@@ -118,31 +118,14 @@ __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
                     w[x] = __builtin_nanf("");
                 }
     };
-    if (in_lds) {
-        // (all loads at once; times stay where they are)
-        f32x4 w[ROUNDS];
-#pragma unroll
-        for (int n = 0; n < ROUNDS; ++n)
-            if (n * STRIDE + 4 * tid < len) {
-                t[n] = *reinterpret_cast<const i32x4*>(time + n * STRIDE + 4 * tid);
-                w[n] = *reinterpret_cast<const f32x4*>(weight + n * STRIDE + 4 * tid);
-            }
-#pragma unroll
-        for (int n = 0; n < ROUNDS; ++n) {
-            const int i = n * STRIDE + 4 * tid;
-            if (i < len) {
-                take_over(i, t[n], w[n]);
-                *reinterpret_cast<u32x4*>(s_rank + i) = u32x4{ordered(w[n][0]), ordered(w[n][1]), ordered(w[n][2]), ordered(w[n][3])};
-                newest = max(max(newest, max(t[n][0], t[n][1])), max(t[n][2], t[n][3]));
-            }
-        }
-    } else {
-        for (int i = 4 * tid; i < len; i += STRIDE) {
-            i32x4 u = *reinterpret_cast<const i32x4*>(time + i);
-            f32x4 w = *reinterpret_cast<const f32x4*>(weight + i);
-            take_over(i, u, w);
-            newest = max(max(newest, max(u[0], u[1])), max(u[2], u[3]));
-        }
+#pragma unroll 4
+    for (int i = 4 * tid; i < len; i += STRIDE) {
+        i32x4 t = *reinterpret_cast<const i32x4*>(time + i);
+        f32x4 w = *reinterpret_cast<const f32x4*>(weight + i);
+        take_over(i, t, w);
+        newest = max(max(newest, max(t[0], t[1])), max(t[2], t[3]));
+        if (in_lds) *reinterpret_cast<u32x4*>(s_rank + i) = u32x4{ordered(w[0]), ordered(w[1]), ordered(w[2]), ordered(w[3])};
+        if (i < STRIDE) t0 = t;
     }
     if (len <= budget) {
         if (tid == 0) a.count[pair] = 0;
@@ -189,14 +172,17 @@ __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
             }
         };
         if (in_lds) {
+#pragma unroll 1
+            for (int i = 4 * tid; i < len; i += STRIDE) {
+                i32x4 t = t0;
+                if (i >= STRIDE) {
+                    t = *reinterpret_cast<const i32x4*>(time + i);
 #pragma unroll
-            for (int n = 0; n < ROUNDS; ++n) {
-                const int i = n * STRIDE + 4 * tid;
-                if (i < len) {
-                    const u32x4 k = ranks_of(t[n], *reinterpret_cast<const u32x4*>(s_rank + i));
-                    *reinterpret_cast<u32x4*>(s_rank + i) = k;
-                    note(k);
+                    for (int x = 1; x < 4; ++x) t[x] = i + x < len ? t[x] : INT32_MIN;
                 }
+                const u32x4 k = ranks_of(t, *reinterpret_cast<const u32x4*>(s_rank + i));
+                *reinterpret_cast<u32x4*>(s_rank + i) = k;
+                note(k);
             }
         } else
             for (int i = 4 * tid; i < len; i += STRIDE) note(ranks(i));
@@ -275,83 +261,68 @@ __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
     least = at_zero ? 0u : least + low;
 
     // Which stay, and where the free slots and the tokens that move into them come in their lists.  Slots come in order of round,
-    // wavefront, lane; as many rounds at a time as counts fit.
+    // wavefront, lane; as many rounds at a time as counts fit: first they are counted, then listed.
+    const int last = budget < len ? budget : len;
     int equals = 0, holes = 0, movers = 0;                     // so far
+#pragma unroll 1
     for (int base = 0; base < len; base += ROUNDS * STRIDE) {
         const int rounds = (len - base + STRIDE - 1) / STRIDE < ROUNDS ? (len - base + STRIDE - 1) / STRIDE : ROUNDS;
-        uint32_t kept = 0, equal = 0;                          // four bits a round
-        int before[ROUNDS];
-#pragma unroll
-        for (int n = 0; n < ROUNDS; ++n) {
-            const int i = base + n * STRIDE + 4 * tid;
-            if (n < rounds && i < len) {
-                const u32x4 k = ranks(i);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    kept |= (uint32_t)(k[x] > least) << (4 * n + x);
-                    equal |= (uint32_t)(k[x] == least) << (4 * n + x);
-                }
-            }
-        }
         if (left > 0) {
-#pragma unroll
-            for (int n = 0; n < ROUNDS; ++n) {
-                if (n < rounds) {
-                    int all;
-                    before[n] = lane_sum_before((int)__popc(equal >> (4 * n) & 15), &all);
-                    if (lane == 0) s_equal[n * WAVES + wave] = all;
-                }
+#pragma unroll 1
+            for (int n = 0; n < rounds; ++n) {
+                const int i = base + n * STRIDE + 4 * tid;
+                const u32x4 k = i < len ? ranks(i) : u32x4{0, 0, 0, 0};
+                int all;
+                lane_sum_before(i < len ? (int)(k[0] == least) + (int)(k[1] == least) + (int)(k[2] == least) + (int)(k[3] == least) : 0, &all);
+                if (lane == 0) s_equal[n * WAVES + wave] = all;
             }
             __syncthreads();
-            const Shares shares(s_equal, rounds * WAVES);
+        }
+        const Shares equal(s_equal, left > 0 ? rounds * WAVES : 0);
+#pragma unroll 1
+        for (int list = 0; list < 2; ++list) {
+            const Shares moves(s_moves, list ? rounds * WAVES : 0);
+#pragma unroll 1
+            for (int n = 0; n < rounds; ++n) {
+                const int i = base + n * STRIDE + 4 * tid, share = n * WAVES + wave;
+                if (list && s_moves[share] == 0) continue;     // nothing of this wavefront's moves
+                const u32x4 k = i < len ? ranks(i) : u32x4{0, 0, 0, 0};
+                uint32_t kept = 0;
 #pragma unroll
-            for (int n = 0; n < ROUNDS; ++n) {
-                if (n < rounds) {
-                    int at_least = equals + shares.before(n * WAVES + wave) + before[n];
+                for (int x = 0; x < 4; ++x) kept |= (uint32_t)(k[x] > least) << x;
+                if (left > 0) {
+                    uint32_t at = 0;
+                    int all;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) at |= (uint32_t)(i < len && k[x] == least) << x;
+                    int before = equals + equal.before(share) + lane_sum_before((int)__popc(at), &all);
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
-                        if (equal >> (4 * n + x) & 1) {
-                            kept |= (uint32_t)(at_least < left) << (4 * n + x);
-                            ++at_least;
-                        }
+                        if (at >> x & 1) kept |= (uint32_t)(before++ < left) << x;
                 }
-            }
-            equals += shares.all;
-        }
-        // both counts in one number: there are 2^15 slots at most
-        const int last = budget < len ? budget : len;
-#pragma unroll
-        for (int n = 0; n < ROUNDS; ++n) {
-            if (n < rounds) {
-                const int i = base + n * STRIDE + 4 * tid;
+                // both counts in one number: there are 2^15 slots at most
                 const uint32_t low4 = i + 4 <= last ? 15u : (i >= last ? 0u : (1u << (last - i)) - 1);
-                const uint32_t k = kept >> (4 * n) & 15;
                 int all;
-                before[n] = lane_sum_before((int)((uint32_t)__popc(low4 & ~k) | (uint32_t)__popc(k & ~low4) << 16), &all);
-                if (lane == 0) s_moves[n * WAVES + wave] = all;
-            }
-        }
-        __syncthreads();
-        const Shares shares(s_moves, rounds * WAVES);
-#pragma unroll
-        for (int n = 0; n < ROUNDS; ++n) {
-            if (n < rounds) {
-                const int i = base + n * STRIDE + 4 * tid;
-                if (s_moves[n * WAVES + wave] != 0) {          // something of this wavefront's moves
-                    const uint32_t both = (uint32_t)before[n] + (uint32_t)shares.before(n * WAVES + wave);
-                    int hole = holes + (int)(both & 0xFFFF), mover = movers + (int)(both >> 16);
+                const uint32_t both = (uint32_t)lane_sum_before((int)((uint32_t)__popc(low4 & ~kept) | (uint32_t)__popc(kept & ~low4) << 16), &all);
+                if (!list) {
+                    if (lane == 0) s_moves[share] = all;
+                } else {
+                    const uint32_t from = both + (uint32_t)moves.before(share);
+                    int hole = holes + (int)(from & 0xFFFF), mover = movers + (int)(from >> 16);
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        const bool stays = kept >> (4 * n + x) & 1;
-                        if (i + x < last && !stays) a.hole[at + hole++] = i + x;
-                        if (i + x >= budget && stays) a.mover[at + mover++] = i + x;
+                        if (low4 & ~kept & 1u << x) a.hole[at + hole++] = i + x;
+                        if (kept & ~low4 & 1u << x) a.mover[at + mover++] = i + x;
                     }
                 }
             }
+            if (list) {
+                holes += moves.all & 0xFFFF;
+                movers += (int)((uint32_t)moves.all >> 16);
+            }
+            __syncthreads();
         }
-        holes += shares.all & 0xFFFF;
-        movers += (int)((uint32_t)shares.all >> 16);
-        __syncthreads();
+        equals += equal.all;
     }
     if (tid == 0) a.count[pair] = movers;
 }
