@@ -21,16 +21,16 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int THREADS = 1024, WAVES = THREADS / 64;
 constexpr int DIGIT = 10, BINS = 1 << DIGIT;      // bits of a digit; a bin a thread
 constexpr int COPIES = 4;                        // of a histogram: lanes that count the same digit do not queue up behind each other
-constexpr int STRIDE = 4 * THREADS, ROUNDS = 8;  // four slots a thread a round
+constexpr int STRIDE = 4 * THREADS;              // slots of all threads, four each
 constexpr int LDS_RANKS = 31744;
-static_assert(BINS == THREADS && LDS_RANKS <= STRIDE * ROUNDS && 2 * 64 == ROUNDS * WAVES, "a bin a thread, two counts a lane");
+static_assert(BINS == THREADS, "a bin a thread");
 
 struct EvictArgs {
     EvictJob j;
     Cache c;
     int32_t *count, *hole, *mover;       // per (sequence, head): how many, their slots (pitch = capacity)
     int copies;                          // weight or time have to be copied where a token stays
-    int room;                            // ranks that LDS holds: up to 4 * ROUNDS a thread
+    int room;                            // ranks that LDS holds
 };
 
 // In the order of the numbers; what is not a number comes first, and zeros are equal.  Rank 0 is for what is below all others: weights that
@@ -52,21 +52,17 @@ __device__ __forceinline__ int lane_sum_before(int v, int* all)
     return (int)((uint32_t)sum - (uint32_t)v);
 }
 
-// Counts of rounds and wavefronts, in that order: what comes before a wavefront's share of each round, and all.
-struct Shares {
-    int one, below;       // of rounds' entries 2 * lane; sum before it
-    int all;
-    __device__ Shares(const int* s_count, int entries)
-    {
-        const int lane = threadIdx.x & 63;
-        one = 2 * lane < entries ? s_count[2 * lane] : 0;
-        below = lane_sum_before((int)((uint32_t)one + (2 * lane < entries ? (uint32_t)s_count[2 * lane + 1] : 0u)), &all);
-    }
-    __device__ int before(int entry) const
-    {
-        return (int)((uint32_t)__builtin_amdgcn_readlane(below, entry >> 1) + (entry & 1 ? (uint32_t)__builtin_amdgcn_readlane(one, entry >> 1) : 0u));
-    }
-};
+// The sum of all lanes of the wavefronts before this one.  All threads take part.
+__device__ __forceinline__ int before_wave(int v, int* s_part, int wave)
+{
+    const int lane = threadIdx.x & 63;
+    int all, none;
+    lane_sum_before(v, &all);
+    __syncthreads();
+    if (lane == 0) s_part[wave] = all;
+    __syncthreads();
+    return __builtin_amdgcn_readlane(lane_sum_before(lane < WAVES ? s_part[lane] : 0, &none), wave);
+}
 
 // ALL_IN_LDS: of every sequence that the cache has room for.  Its 1024 threads take 8.5 us for 8 heads of 2 358 tokens (512: 9.1, 256: 10.3), mostly
 // the latency of about 20 steps that follow from each other, and 25 us for 128 heads of 17 000 - 25 000.
@@ -75,7 +71,7 @@ __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
 {
     extern __shared__ __align__(16) uint32_t s_rank[];
     __shared__ __align__(16) int hist[BINS * COPIES];
-    __shared__ int s_part[WAVES], s_equal[ROUNDS * WAVES], s_moves[ROUNDS * WAVES];
+    __shared__ int s_part[WAVES];
     __shared__ int s_newest, s_recent, s_pick[3];
     __shared__ uint32_t s_low, s_high;
     const Cache& c = a.c;
@@ -136,8 +132,8 @@ __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
     if (lane == 0) atomicMax(&s_newest, newest);
     __syncthreads();
     // times from here on are recent, if any are
-    const long from = (long)s_newest - a.j.window + 1;
-    const int recent_from = from < INT32_MIN ? INT32_MIN : (from > INT32_MAX ? INT32_MAX : (int)from);
+    const long earliest = (long)s_newest - a.j.window + 1;
+    const int recent_from = earliest < INT32_MIN ? INT32_MIN : (earliest > INT32_MAX ? INT32_MAX : (int)earliest);
     const bool any_recent = a.j.window > 0;
     bool by_time = false;
     auto ranks_of = [&](const i32x4& t, const u32x4& of_weight) {
@@ -260,71 +256,64 @@ __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
     }
     least = at_zero ? 0u : least + low;
 
-    // Which stay, and where the free slots and the tokens that move into them come in their lists.  Slots come in order of round,
-    // wavefront, lane; as many rounds at a time as counts fit: first they are counted, then listed.
-    const int last = budget < len ? budget : len;
-    int equals = 0, holes = 0, movers = 0;                     // so far
+    // Which stay, and where the free slots and the tokens that move into them come in their lists.  A wavefront has a stretch of slots, 256 at
+    // a time: first all count theirs, then they list them.
+    const int last = budget < len ? budget : len, stretch = (len + STRIDE - 1) / STRIDE * 256;
+    const int from = wave * stretch < len ? wave * stretch : len, to = from + stretch < len ? from + stretch : len;
+    int equal = 0, hole = 0, mover = 0;                        // before this wavefront's, then before the slots that come
+    if (left > 0) {
 #pragma unroll 1
-    for (int base = 0; base < len; base += ROUNDS * STRIDE) {
-        const int rounds = (len - base + STRIDE - 1) / STRIDE < ROUNDS ? (len - base + STRIDE - 1) / STRIDE : ROUNDS;
-        if (left > 0) {
-#pragma unroll 1
-            for (int n = 0; n < rounds; ++n) {
-                const int i = base + n * STRIDE + 4 * tid;
-                const u32x4 k = i < len ? ranks(i) : u32x4{0, 0, 0, 0};
-                int all;
-                lane_sum_before(i < len ? (int)(k[0] == least) + (int)(k[1] == least) + (int)(k[2] == least) + (int)(k[3] == least) : 0, &all);
-                if (lane == 0) s_equal[n * WAVES + wave] = all;
-            }
-            __syncthreads();
+        for (int i = from + 4 * lane; i < to; i += 256) {
+            const u32x4 k = ranks(i);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) equal += i + x < len && k[x] == least;
         }
-        const Shares equal(s_equal, left > 0 ? rounds * WAVES : 0);
-#pragma unroll 1
-        for (int list = 0; list < 2; ++list) {
-            const Shares moves(s_moves, list ? rounds * WAVES : 0);
-#pragma unroll 1
-            for (int n = 0; n < rounds; ++n) {
-                const int i = base + n * STRIDE + 4 * tid, share = n * WAVES + wave;
-                if (list && s_moves[share] == 0) continue;     // nothing of this wavefront's moves
-                const u32x4 k = i < len ? ranks(i) : u32x4{0, 0, 0, 0};
-                uint32_t kept = 0;
-#pragma unroll
-                for (int x = 0; x < 4; ++x) kept |= (uint32_t)(k[x] > least) << x;
-                if (left > 0) {
-                    uint32_t at = 0;
-                    int all;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) at |= (uint32_t)(i < len && k[x] == least) << x;
-                    int before = equals + equal.before(share) + lane_sum_before((int)__popc(at), &all);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        if (at >> x & 1) kept |= (uint32_t)(before++ < left) << x;
-                }
-                // both counts in one number: there are 2^15 slots at most
-                const uint32_t low4 = i + 4 <= last ? 15u : (i >= last ? 0u : (1u << (last - i)) - 1);
-                int all;
-                const uint32_t both = (uint32_t)lane_sum_before((int)((uint32_t)__popc(low4 & ~kept) | (uint32_t)__popc(kept & ~low4) << 16), &all);
-                if (!list) {
-                    if (lane == 0) s_moves[share] = all;
-                } else {
-                    const uint32_t from = both + (uint32_t)moves.before(share);
-                    int hole = holes + (int)(from & 0xFFFF), mover = movers + (int)(from >> 16);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        if (low4 & ~kept & 1u << x) a.hole[at + hole++] = i + x;
-                        if (kept & ~low4 & 1u << x) a.mover[at + mover++] = i + x;
-                    }
-                }
-            }
-            if (list) {
-                holes += moves.all & 0xFFFF;
-                movers += (int)((uint32_t)moves.all >> 16);
-            }
-            __syncthreads();
-        }
-        equals += equal.all;
+        equal = before_wave(equal, s_part, wave);
     }
-    if (tid == 0) a.count[pair] = movers;
+#pragma unroll 1
+    for (int list = 0; list < 2; ++list) {
+        int run = equal;
+#pragma unroll 1
+        for (int i0 = from; i0 < to; i0 += 256) {
+            const int i = i0 + 4 * lane;
+            const u32x4 k = i < to ? ranks(i) : u32x4{0, 0, 0, 0};
+            uint32_t kept = 0;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) kept |= (uint32_t)(k[x] > least) << x;
+            if (left > 0) {
+                int own = 0, all;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) own += i + x < to && k[x] == least;
+                int at_least = run + lane_sum_before(own, &all);
+                run += all;
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    if (i + x < to && k[x] == least) kept |= (uint32_t)(at_least++ < left) << x;
+            }
+            const uint32_t low4 = i + 4 <= last ? 15u : (i >= last ? 0u : (1u << (last - i)) - 1);
+            const uint32_t holes = low4 & ~kept, movers = kept & ~low4;
+            if (!list) {
+                hole += (int)__popc(holes);
+                mover += (int)__popc(movers);
+            } else if (__ballot(holes | movers)) {
+                int all;                                       // (both counts in one number)
+                const int before = lane_sum_before((int)(__popc(holes) | __popc(movers) << 16), &all);
+                int h_at = hole + (before & 0xFFFF), m_at = mover + (before >> 16);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    if (holes >> x & 1) a.hole[at + h_at++] = i + x;
+                    if (movers >> x & 1) a.mover[at + m_at++] = i + x;
+                }
+                hole += all & 0xFFFF;
+                mover += all >> 16;
+            }
+        }
+        if (!list) {
+            hole = before_wave(hole, s_part, wave);
+            mover = before_wave(mover, s_part, wave);
+        }
+    }
+    if (wave == WAVES - 1 && lane == 0) a.count[pair] = mover;
 }
 
 // Moves: 16-byte pieces of keys and values, weight and time; the sequences' lengths.
@@ -382,9 +371,10 @@ hipError_t launch_evict(const EvictJob& j, const Cache& c, hipStream_t st)
     else hipLaunchKernelGGL(select_kernel<false>, grid, block, a.room * 4, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    // workgroups of the moves: a few for each compute unit, no more than the most there can be to move
+    // workgroups of the moves: 64 for each compute unit (128 heads of 3 000 tokens each: 102 us with 8, 91 with 64), no more than the most there
+    // can be to move
     const long most = ((long)(c.capacity - j.budget < j.budget ? c.capacity - j.budget : j.budget) * (c.dim * (c.bf16 ? 2 : 4) / 16) + 255) / 256;
-    long per = (8L * device_units() + pairs - 1) / pairs;
+    long per = (64L * device_units() + pairs - 1) / pairs;
     per = per > most ? most : per;
     hipLaunchKernelGGL(move_kernel, dim3((unsigned)(per < 1 ? 1 : per), c.heads, c.seqs), dim3(256), 0, st, a);
     return hipGetLastError();
