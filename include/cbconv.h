@@ -454,7 +454,7 @@ int cb_cache_scratch_bytes(const cb_cache *cache, int32_t n_q_heads, size_t *byt
  * kept.  rotary not NULL: keys are rotated on the way, and q into q_out if q is not NULL (whose row n
  * belongs to row n of k).  positions_dev: n_tokens x n_axes (n_tokens x 1 without rotary; NULL there: a token's time is its
  * slot).  weight becomes 0, time the position on axis 0.  Rows from offsets_dev[n_seq] on are ignored, q's too, so
- * that n_tokens may be an upper bound of a count that only the device knows. */
+ * that n_tokens (below 2^24) may be an upper bound of a count that only the device knows. */
 int cb_cache_append(const cb_cache *cache, const cb_rotary *rotary, int32_t n_tokens, const int32_t *positions_dev,
                     const int32_t *offsets_dev, const int32_t *start_dev, const cb_heads *k, const cb_heads *v,
                     const cb_heads *q, const cb_heads *q_out, void *hip_stream);
@@ -464,7 +464,8 @@ int cb_cache_append(const cb_cache *cache, const cb_rotary *rotary, int32_t n_to
  * q->heads is a multiple of n_kv_heads; query head i reads key head i / (q->heads / n_kv_heads).  lse_dev (may be NULL): n_seq x
  * q->heads float32, ln of the sum.  A sequence without a token, or with scores of minus infinity alone, gives zeros and minus
  * infinity.  n_seq * capacity * (key heads times blocks of 16 of their query heads) stays below 2^35.  accumulate = 1 (weight_dev not NULL): weight becomes decay * weight + the sum over the query heads that read it of
- * e^(s_j - lse), for every slot that holds a token.  The sums' order depends on lengths and sizes alone. */
+ * e^(s_j - lse), for every slot that holds a token.  The order of the sums depends on
+ * lengths, sizes and the GPU's compute units alone.  out overlaps no other array. */
 typedef struct {
     float scale, softcap;      /* finite; softcap >= 0, 0: none */
     float decay;               /* 0 .. 1 */

@@ -279,10 +279,19 @@ hipError_t launch(const RotaryJob& j, const Cache& c, int lengths, hipStream_t s
 
 }  // namespace
 
-hipError_t launch_rotate(const RotaryJob& j, hipStream_t st)
+// (a launch has fewer than 2^32 threads: at most MOST_TOKENS tokens with a workgroup each)
+hipError_t launch_rotate(const RotaryJob& all, hipStream_t st)
 {
-    if (j.tokens == 0 || j.q.heads + j.k.heads == 0) return hipSuccess;
-    return launch<false>(j, Cache(), LENGTHS_LATER, st);
+    const long size = all.bf16 ? 2 : 4;
+    for (long at = 0; at < all.tokens; at += MOST_TOKENS) {
+        RotaryJob j = all;
+        j.tokens = all.tokens - at < MOST_TOKENS ? all.tokens - at : MOST_TOKENS;
+        j.positions += at * j.pos_axes;
+        for (Heads* h : {&j.q, &j.q_out, &j.k, &j.k_out}) h->data = (const char*)h->data + at * h->token * size;
+        const hipError_t e = launch<false>(j, Cache(), LENGTHS_LATER, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // lengths of the cache are written by the first workgroup where start is another array; where it is the same one, by the

@@ -54,6 +54,7 @@ struct RotaryJob {
     // append
     const int32_t *offsets, *start;
 };
+constexpr long MOST_TOKENS = (1L << 24) - 1;      // of a launch
 hipError_t launch_rotate(const RotaryJob& j, hipStream_t st);
 hipError_t launch_append(const RotaryJob& j, const Cache& c, hipStream_t st);
 

@@ -170,7 +170,7 @@ int cb_cache_append(const cb_cache* cache, const cb_rotary* rotary, int32_t n_to
     cb::Cache c = {};
     CB_CHECKED(cb::check_cache(cache, true, 0, &c));
     const int dtype = cache->dtype;
-    if (n_tokens < 0 || (!offsets_dev && n_tokens != c.seqs)) return CB_EINVAL;
+    if (n_tokens < 0 || n_tokens > cb::MOST_TOKENS || (!offsets_dev && n_tokens != c.seqs)) return CB_EINVAL;
     const bool empty = n_tokens == 0;
     if (q && (!rotary || !q_out)) return CB_EINVAL;
     if (!q && q_out) return CB_EINVAL;

@@ -149,6 +149,19 @@ def test_rotate_nothing():
     assert rot.rotate(q, torch.empty((0, 1), dtype=torch.int32, device="cuda")).shape == (0, 3, 16)
 
 
+def test_rotate_more_tokens_than_a_launch_takes():
+    """Of more than 2^24 tokens the last ones are turned as the same tokens by themselves."""
+    n, dim, pairs = (1 << 24) + 1000, 8, (1, 1, 2)
+    q = torch.randn((n, 1, dim), device="cuda").to(BF16)
+    pos = torch.randint(0, 1000, (n, 3), device="cuda", dtype=torch.int32)
+    rot = cb.Rotary(dim, pairs)
+    got = rot.rotate(q, pos, k=q)
+    for at in (0, (1 << 24) - 500, n - 700):
+        want = rot.rotate(q[at:at + 700], pos[at:at + 700].contiguous())
+        for x in got:
+            assert torch.equal(x[at:at + 700], want)
+
+
 # ---------------------------------------------------------------- caches
 def make_cache(rng, lengths, heads, dim, page, dtype, capacity=None, spare=3, evictable=True, fill=math.nan):
     """A cache whose pages lie in no order; slots that hold no token are `fill`, and so are pages of nobody."""

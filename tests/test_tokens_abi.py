@@ -98,7 +98,8 @@ BAD_CACHES = [dict(n_seq=0), dict(n_seq=65536), dict(n_kv_heads=0), dict(n_kv_he
               dict(head_dim=264), dict(page_tokens=8), dict(page_tokens=48), dict(page_tokens=2048), dict(max_pages=0),
               dict(max_pages=1 << 27), dict(n_pages=0), dict(dtype=2), dict(reserved=1)]
 BAD_BUFFERS = [dict(k_pages_dev=None), dict(v_pages_dev=None), dict(k_pages_dev=FAKE + 8), dict(v_pages_dev=FAKE + 4),
-               dict(table_dev=None), dict(lengths_dev=None), dict(scratch_dev=None), dict(scratch_dev=FAKE + 128)]
+               dict(table_dev=None), dict(lengths_dev=None), dict(scratch_dev=None), dict(scratch_dev=FAKE + 128),
+               dict(weight_dev=FAKE + 4), dict(time_dev=FAKE + 8)]
 
 
 @pytest.mark.parametrize("kw", BAD_CACHES)
@@ -130,7 +131,7 @@ def test_append_refusals():
 
     bad = rotary()
     bad.desc.base = 0.0
-    for kw in (dict(c=None), dict(rot=bad), dict(rot=rotary(head_dim=80)), dict(n=-1, off=FAKE), dict(n=3), dict(pos=None), dict(k=None),
+    for kw in (dict(c=None), dict(rot=bad), dict(rot=rotary(head_dim=80)), dict(n=-1, off=FAKE), dict(n=1 << 24, off=FAKE), dict(n=3), dict(pos=None), dict(k=None),
                dict(v=None), dict(k=heads(2)), dict(v=heads(5)), dict(qo=None), dict(q=None), dict(qo=heads(4)), dict(rot=None),
                dict(k=heads(data=None)), dict(v=heads(data=FAKE + 1)), dict(q=heads(8, reserved=3))):
         assert call(**kw) == cb.CB_EINVAL, kw
@@ -163,6 +164,15 @@ def test_evict_refusals():
         p = binding.cb_evict_params(budget, window, None, None, None)
         assert L.cb_cache_evict(None if c is None else C.byref(c), C.byref(p), None) == cb.CB_EINVAL
     assert L.cb_cache_evict(C.byref(cache()), None, None) == cb.CB_EINVAL
+    for bad in (binding.cb_evict_params(8, 0, FAKE + 4, None, None), binding.cb_evict_params(8, 0, None, FAKE + 8, None)):
+        assert L.cb_cache_evict(C.byref(cache()), C.byref(bad), None) == cb.CB_EINVAL
+
+
+def test_attention_whose_work_is_not_counted_in_32_bits_is_refused():
+    L, p = binding.lib(), binding.cb_attend_params(1.0, 0.0, 1.0, 0, 0)
+    for kw in (dict(n_seq=65535, n_kv_heads=4, max_pages=1 << 13, page_tokens=1024), dict(n_seq=4, max_pages=1 << 20, page_tokens=1024)):
+        c = cache(weight_dev=None, scratch_bytes=1 << 62, **kw)
+        assert L.cb_cache_attend(C.byref(c), C.byref(p), C.byref(heads(512)), C.byref(heads(512)), None, None) == cb.CB_EINVAL
 
 
 def test_scratch_sizes():
