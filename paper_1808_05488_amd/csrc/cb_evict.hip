@@ -22,7 +22,7 @@ constexpr int THREADS = 1024, WAVES = THREADS / 64;
 constexpr int DIGIT = 10, BINS = 1 << DIGIT;      // bits of a digit; a bin a thread
 constexpr int COPIES = 4;                        // of a histogram: lanes that count the same digit do not queue up behind each other
 constexpr int STRIDE = 4 * THREADS;              // slots of all threads, four each
-constexpr int LDS_RANKS = 31744;
+constexpr int LDS_RANKS = 30720;
 static_assert(BINS == THREADS, "a bin a thread");
 
 struct EvictArgs {
@@ -52,16 +52,12 @@ __device__ __forceinline__ int lane_sum_before(int v, int* all)
     return (int)((uint32_t)sum - (uint32_t)v);
 }
 
-// The sum of all lanes of the wavefronts before this one.  All threads take part.
-__device__ __forceinline__ int before_wave(int v, int* s_part, int wave)
+// The sum of all wavefronts' entries before this one's.
+__device__ __forceinline__ int before_wave(const int* s_part, int wave)
 {
     const int lane = threadIdx.x & 63;
-    int all, none;
-    lane_sum_before(v, &all);
-    __syncthreads();
-    if (lane == 0) s_part[wave] = all;
-    __syncthreads();
-    return __builtin_amdgcn_readlane(lane_sum_before(lane < WAVES ? s_part[lane] : 0, &none), wave);
+    int all;
+    return __builtin_amdgcn_readlane(lane_sum_before(lane < WAVES ? s_part[lane] : 0, &all), wave);
 }
 
 // ALL_IN_LDS: of every sequence that the cache has room for.  Its 1024 threads take 8.5 us for 8 heads of 2 358 tokens (512: 9.1, 256: 10.3), mostly
@@ -70,8 +66,8 @@ template <bool ALL_IN_LDS>
 __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
 {
     extern __shared__ __align__(16) uint32_t s_rank[];
-    __shared__ __align__(16) int hist[BINS * COPIES];
-    __shared__ int s_part[WAVES];
+    __shared__ __align__(16) int hist[2][BINS * COPIES];     // of this digit, and the next one's, empty
+    __shared__ int s_part[WAVES], s_equal[WAVES], s_hole[WAVES], s_mover[WAVES];
     __shared__ int s_newest, s_recent, s_pick[3];
     __shared__ uint32_t s_low, s_high;
     const Cache& c = a.c;
@@ -87,6 +83,7 @@ __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
         s_low = 0xFFFFFFFFu;
         s_high = 0;
     }
+    *reinterpret_cast<i32x4*>(hist[0] + 4 * tid) = i32x4{0, 0, 0, 0};
     // Times and weights, four slots a thread (a row ends behind a multiple of 16).  Where others than the cache's own decide, the cache
     // receives them: of free slots too, which the moves write over.
     const bool in_lds = ALL_IN_LDS || len <= a.room;
@@ -205,10 +202,10 @@ __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
     uint32_t least = 0;
     int shift = 32 - __builtin_clz(range | 1) - DIGIT;
 #pragma unroll 1
-    for (int past = 32; s_high != 0;) {
+    for (int past = 32, turn = 0; s_high != 0; turn ^= 1) {
+        int* counts = hist[turn];
         shift = shift < 0 ? 0 : shift;
-        *reinterpret_cast<i32x4*>(hist + 4 * tid) = i32x4{0, 0, 0, 0};
-        __syncthreads();
+        *reinterpret_cast<i32x4*>(hist[turn ^ 1] + 4 * tid) = i32x4{0, 0, 0, 0};
         // (recent tokens are out of range but where the range ends with them: then there are none)
 #pragma unroll 2
         for (int i = 4 * tid; i < len; i += STRIDE) {
@@ -217,13 +214,13 @@ __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
             for (int x = 0; x < 4; ++x) {
                 const uint32_t k = r[x] - low;
                 if (k <= range && (past == 32 || (k ^ least) >> past == 0))
-                    atomicAdd(&hist[((k >> shift) & (BINS - 1)) * COPIES + (lane & (COPIES - 1))], 1);
+                    atomicAdd(&counts[((k >> shift) & (BINS - 1)) * COPIES + (lane & (COPIES - 1))], 1);
             }
         }
         __syncthreads();
         // from the highest digit down, a digit a thread
         const int digit = BINS - 1 - tid;
-        const i32x4 bin = *reinterpret_cast<const i32x4*>(hist + digit * COPIES);
+        const i32x4 bin = *reinterpret_cast<const i32x4*>(counts + digit * COPIES);
         const int n = bin[0] + bin[1] + bin[2] + bin[3];
         int all, counted;
         int above = lane_sum_before(n, &all);
@@ -268,7 +265,11 @@ __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
 #pragma unroll
             for (int x = 0; x < 4; ++x) equal += i + x < len && k[x] == least;
         }
-        equal = before_wave(equal, s_part, wave);
+        int all;
+        lane_sum_before(equal, &all);
+        if (lane == 0) s_equal[wave] = all;
+        __syncthreads();
+        equal = before_wave(s_equal, wave);
     }
 #pragma unroll 1
     for (int list = 0; list < 2; ++list) {
@@ -309,8 +310,13 @@ __global__ __launch_bounds__(THREADS) void select_kernel(const EvictArgs a)
             }
         }
         if (!list) {
-            hole = before_wave(hole, s_part, wave);
-            mover = before_wave(mover, s_part, wave);
+            int holes, movers;
+            lane_sum_before(hole, &holes);
+            lane_sum_before(mover, &movers);
+            if (lane == 0) { s_hole[wave] = holes; s_mover[wave] = movers; }
+            __syncthreads();
+            hole = before_wave(s_hole, wave);
+            mover = before_wave(s_mover, wave);
         }
     }
     if (wave == WAVES - 1 && lane == 0) a.count[pair] = mover;
