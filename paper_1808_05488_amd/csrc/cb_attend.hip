@@ -2,7 +2,8 @@
 //
 // For each sequence and key head: s_j = scale q.k_j for the query heads that read the key head, the softmax over the
 // cached tokens j, and the weighted sum of the v_j.  Keys and values are read once, so memory bounds it: 4 * dim * heads operations for
-// 2 * dim * heads / group values.  One pass: every wavefront takes tiles of consecutive tokens and keeps, for up to 16 query heads, the running maximum m,
+// 2 * dim * heads / group values (200 003 tokens of 8 key heads, 128 values in bfloat16: 131 us, 6.2 TB/s, where plain reads reach 7.2; 6.5 over
+// 32 x 8 192 tokens).  One pass: every wavefront takes tiles of consecutive tokens and keeps, for up to 16 query heads, the running maximum m,
 // the sum l of e^(s - m) and the sum o of e^(s - m) v; a tile with a larger maximum scales l and o by e^(m - m').  Parts of a sequence (wavefronts of
 // a workgroup, then workgroups) are joined the same way.
 //
@@ -652,7 +653,9 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
     }
 }
 
-// weight = decay * weight + the sum over the query heads of a key head of e^(s - lse), four slots a thread.
+// weight = decay * weight + the sum over the query heads of a key head of e^(s - lse), four slots a thread.  A launch of its own, since lse is
+// only known when all parts are joined: the scores wait in the scratch buffer (4 bytes a query head where keys and values are 4 * dim;
+// 24 sequences of 51 000 tokens in all, 32 query heads: 5 us here, 10 us of the 57 with the scores' way and the launch).
 __global__ __launch_bounds__(256) void weight_kernel(const AttendArgs a)
 {
     const int seq = blockIdx.z, h = blockIdx.y, slot = (blockIdx.x * 256 + threadIdx.x) * 4, len = clamp_length(a.c.lengths[seq], a.c.capacity);
