@@ -692,7 +692,8 @@ class TokenCache:
 
     k_pages, v_pages: pages x key heads x page_tokens x head_dim; table: sequences x pages of a sequence, int32; lengths:
     sequences, int32; weight (float32) and time (int32): sequences x key heads x capacity, needed to evict.  Calls run on
-    the current stream; calls that share a cache or a scratch buffer have to be on one stream, or ordered."""
+    the current stream; calls that share a cache or a scratch buffer have to be on one stream, or ordered.  A graph that
+    has recorded calls needs the object as long as it is replayed: its scratch buffers stay until then."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
                  weight: Optional[torch.Tensor] = None, time: Optional[torch.Tensor] = None,
@@ -715,6 +716,7 @@ class TokenCache:
         self.k_pages, self.v_pages, self.table, self.lengths, self.weight, self.time = k_pages, v_pages, table, lengths, weight, time
         self._address = C.addressof(d)
         self._room = -1                    # query heads that the scratch buffer has room for
+        self._outgrown = []                # scratch buffers that graphs and other streams may still use
         self._lse = {}                     # by query heads: what an lse is like
         self._scratch(0, scratch)
 
@@ -741,8 +743,13 @@ class TokenCache:
         if given is None and self._room >= 0 and self.scratch.numel() >= nbytes:
             given = self.scratch
         if given is None:
+            # its counters are cleared once, now: a recorded clearing would only come with the graph's first replay
+            assert not torch.cuda.is_current_stream_capturing(), \
+                f"a scratch buffer for {n_q_heads} query heads has to be made before a graph is recorded: attend once before, or give one"
             given = _alloc(nbytes, self.device)
             given.zero_()
+            if self._room >= 0:
+                self._outgrown.append(self.scratch)
         assert given.dtype == torch.uint8 and given.device == self.device and given.is_contiguous()
         self.scratch, self._room = given, n_q_heads
         self.desc.scratch_dev, self.desc.scratch_bytes = given.data_ptr(), given.numel()

@@ -768,3 +768,43 @@ def test_what_python_refuses():
         cb.TokenCache(c.k_pages, c.v_pages, c.table.long(), c.lengths)
     with pytest.raises(cb.CBError):
         cb.TokenCache(c.k_pages.view(8, 2, 16, 32)[:, :, :8].contiguous(), c.v_pages[:, :, :8].contiguous(), c.table, c.lengths)
+
+
+def test_a_graph_keeps_the_scratch_buffer_that_it_was_recorded_with():
+    rng = np.random.default_rng(42)
+    c = make_cache(rng, [5000, 40], 2, 64, 64, BF16)
+    q, more = (dev(rng.standard_normal((2, heads, 64)), BF16) for heads in (4, 32))
+    want, want_lse = c.attend(q)
+    out, lse = torch.zeros_like(want), torch.zeros_like(want_lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.attend(q, out=out, lse=lse)
+    nbytes = c.scratch.numel()
+    wider = c.attend(more)[0]
+    assert c.scratch.numel() > nbytes
+    others = [torch.full((nbytes + 256,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(4)]      # would take a buffer that is free
+    for _ in range(3):
+        out.zero_()
+        lse.zero_()
+        graph.replay()
+        assert torch.equal(c.attend(more)[0], wider)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    assert all(bool((x == 0x5A).all()) for x in others)
+
+
+def test_no_scratch_buffer_is_made_while_a_graph_is_recorded():
+    rng = np.random.default_rng(43)
+    c = make_cache(rng, [300, 40], 2, 64, 64, BF16)
+    q = dev(rng.standard_normal((2, 32, 64)), BF16)
+    x = torch.zeros(8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x.add_(1.0)
+        with pytest.raises(AssertionError, match="attend once before"):
+            c.attend(q)
+    want = c.attend(q)[0]
+    graph.replay()
+    assert torch.equal(c.attend(q)[0], want) and bool((x == 1).all())
