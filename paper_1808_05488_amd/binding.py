@@ -771,7 +771,7 @@ class TokenCache:
             else:
                 d = _heads(q_out, "q_out", dtype, i, dim, q.shape[1], n)
         status = lib().cb_cache_append(
-            self._address, None if rotary is None else rotary._address, n,
+            self._address, None if rotary is None else rotary._address, n if n < 2 ** 31 else -1,
             _dense(positions, "positions", torch.int32, i, (n, 1 if rotary is None else rotary.n_axes)),
             _dense(offsets, "offsets", torch.int32, i, (self.n_seq + 1,)), _dense(start, "start", torch.int32, i, (self.n_seq,)),
             a, b, c, d, _raw_stream(i))

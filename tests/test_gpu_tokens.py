@@ -808,3 +808,11 @@ def test_no_scratch_buffer_is_made_while_a_graph_is_recorded():
     want = c.attend(q)[0]
     graph.replay()
     assert torch.equal(c.attend(q)[0], want) and bool((x == 1).all())
+
+
+def test_append_refuses_more_rows_than_its_count_holds():
+    c = cb.TokenCache.create(2, 2, 32, 64, F32, 16)
+    rows = torch.zeros((1, 2, 32), device="cuda").expand(2 ** 32 + 2, 2, 32)       # 2 rows, were the count cut to 32 bits
+    with pytest.raises(cb.CBError):
+        c.append(rows, rows)
+    assert not bool(c.lengths.any())
