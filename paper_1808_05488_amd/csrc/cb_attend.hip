@@ -387,12 +387,25 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                     l += p[s][r];
                 }
             if constexpr (HALF) {
-                // P in two bfloat16 terms: one alone would round as much as the result's own rounding does
-                bf16x8 hi, lo;
+                // P in three bfloat16 terms of 8 significant bits each, cut off and not rounded: they hold all of a float32's 24 bits, so that P is
+                // no less exact than in float32 (two terms put the sums off by 2^-18 of the values; the third one costs nothing: memory bounds the tile)
+                uint32_t cut[3][8];
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
-                    hi[x] = (__bf16)p[x / 4][x % 4];
-                    lo[x] = (__bf16)(p[x / 4][x % 4] - (float)hi[x]);
+                    float rest = p[x / 4][x % 4];
+#pragma unroll
+                    for (int y = 0; y < 3; ++y) {
+                        cut[y][x] = __float_as_uint(rest) & 0xFFFF0000u;
+                        rest -= __uint_as_float(cut[y][x]);
+                    }
+                }
+                bf16x8 terms[3];
+#pragma unroll
+                for (int y = 0; y < 3; ++y) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) w[x] = __builtin_amdgcn_perm(cut[y][2 * x + 1], cut[y][2 * x], 0x07060302u);
+                    terms[y] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
                 }
 #pragma unroll
                 for (int pc = 0; pc < NP; ++pc)
@@ -407,8 +420,8 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                             w[x] = __builtin_amdgcn_perm(v[s][r + 1][pc][e / 2], v[s][r][pc][e / 2], sel);
                         }
                         const bf16x8 vt = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-                        o[pc * PE + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, hi, o[pc * PE + e], 0, 0, 0);
-                        o[pc * PE + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, lo, o[pc * PE + e], 0, 0, 0);
+#pragma unroll
+                        for (int y = 0; y < 3; ++y) o[pc * PE + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, terms[y], o[pc * PE + e], 0, 0, 0);
                     }
             } else {
 #pragma unroll

@@ -816,3 +816,29 @@ def test_append_refuses_more_rows_than_its_count_holds():
     with pytest.raises(cb.CBError):
         c.append(rows, rows)
     assert not bool(c.lengths.any())
+
+
+def small_cache(k, v, page=16, weight=False):
+    """A cache of one head whose sequences hold k and v (sequences x tokens x dim)."""
+    n_seq, n, dim = k.shape
+    c = cb.TokenCache.create(n_seq, 1, dim, n, k.dtype, page, evictable=weight)
+    c.append(k.reshape(-1, 1, dim), v.reshape(-1, 1, dim), offsets=torch.arange(0, n_seq * n + 1, n, dtype=torch.int32, device="cuda"))
+    return c
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_attend_weights_keep_the_bits_of_float32(dim):
+    """Two tokens whose values nearly cancel, each in its own way: what is left shows the weights' own rounding."""
+    b, heads = 8, 16
+    k = torch.zeros((b, 2, dim), dtype=BF16, device="cuda")
+    k[:, 1, 0] = -1.0
+    v = torch.ones((b, 2, dim), dtype=BF16, device="cuda")
+    v[:, 1] = -(1 + (torch.arange(dim, device="cuda") % 64) / 64).to(BF16)
+    c = small_cache(k, v)
+    q = torch.zeros((b, heads, dim), dtype=BF16, device="cuda")
+    q[..., 0] = (1 + torch.arange(b * heads, device="cuda").view(b, heads) / 128).to(BF16)          # 128 numbers of 8 bits
+    out, _ = c.attend(q, scale=0.25)
+    p = np.exp(-0.25 * f64(q)[..., 0])[..., None]       # (of exact scores)
+    want = (1 + p * f64(v)[0, 1]) / (1 + p)
+    # of sums of up to 2: a weight to 1.5 units in its last place (3 EPS of values up to 2), three sums (2 EPS each), over 1.6; and the result's rounding
+    within(f64(out), want, 8 * EPS + ROUND[BF16] * np.abs(want), "out")
