@@ -18,12 +18,15 @@
 // whole it finishes, and what begins or ends in the middle of something waits in LDS until all wavefronts are through.  What
 // begins or ends in the middle of something for the workgroup goes to the scratch buffer, and the workgroup that comes last of those that
 // share it joins the parts, in order.
+#include <type_traits>
+
 #include "cb_tokens.h"
 
 namespace cb {
 
 namespace {
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -46,6 +49,13 @@ struct AttendArgs {
 
 // e^x for the difference x of two scores, which is exact or nearly so; scores times log2 e would be rounded at their own size.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
+
+// Two bfloat16 values, zero in the place of one that is not finite.
+__device__ __forceinline__ uint32_t finite_halves(uint32_t w)
+{
+    const uint32_t odd = ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;       // of a half whose exponent is all ones
+    return w & ~(odd | (odd - (odd >> 15)));
+}
 
 // Part of (sequence, key head, block of query heads) in the scratch buffer: ROWS maxima, ROWS sums, ROWS x DP values.
 template <int DP> constexpr int part_floats() { return ROWS * (DP + 2); }
@@ -407,22 +417,44 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                     for (int x = 0; x < 4; ++x) w[x] = __builtin_amdgcn_perm(cut[y][2 * x + 1], cut[y][2 * x], 0x07060302u);
                     terms[y] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
                 }
+                // The lower terms may be zero where P is not, and zero times infinity is not a number: where a tile has values that are not
+                // finite (rare, and one question for 64 lanes), the first term alone meets them.
+                u16x2 size = {0, 0};                           // the largest exponents, of both halves of the words
 #pragma unroll
-                for (int pc = 0; pc < NP; ++pc)
+                for (int s = 0; s < SUB; ++s)
 #pragma unroll
-                    for (int e = 0; e < PE; ++e) {
-                        // value e of the eight tokens, in the order that P has them in
-                        uint32_t w[4];
-                        const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+                    for (int r = 0; r < 4; ++r)
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const int s = x / 2, r = 2 * (x % 2);
-                            w[x] = __builtin_amdgcn_perm(v[s][r + 1][pc][e / 2], v[s][r][pc][e / 2], sel);
+                        for (int pc = 0; pc < NP; ++pc)
+#pragma unroll
+                            for (int x = 0; x < DW; ++x) size = __builtin_elementwise_max(size, __builtin_bit_cast(u16x2, v[s][r][pc][x] & 0x7F807F80u));
+                auto add_values = [&](auto all_finite) {
+#pragma unroll
+                    for (int pc = 0; pc < NP; ++pc)
+#pragma unroll
+                        for (int e = 0; e < PE; ++e) {
+                            // value e of the eight tokens, in the order that P has them in
+                            uint32_t w[4];
+                            const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                const int s = x / 2, r = 2 * (x % 2);
+                                w[x] = __builtin_amdgcn_perm(v[s][r + 1][pc][e / 2], v[s][r][pc][e / 2], sel);
+                            }
+                            bf16x8 vt = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+                            for (int y = 0; y < 3; ++y) {
+                                o[pc * PE + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, terms[y], o[pc * PE + e], 0, 0, 0);
+                                if (!all_finite.value && y == 0) {
+#pragma unroll
+                                    for (int x = 0; x < 4; ++x) w[x] = finite_halves(w[x]);
+                                    vt = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+                                }
+                            }
                         }
-                        const bf16x8 vt = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-#pragma unroll
-                        for (int y = 0; y < 3; ++y) o[pc * PE + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, terms[y], o[pc * PE + e], 0, 0, 0);
-                    }
+                };
+                if (__ballot(size[0] == 0x7F80 || size[1] == 0x7F80)) add_values(std::false_type());
+                else add_values(std::true_type());
             } else {
 #pragma unroll
                 for (int pc = 0; pc < NP; ++pc)

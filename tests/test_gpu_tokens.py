@@ -842,3 +842,30 @@ def test_attend_weights_keep_the_bits_of_float32(dim):
     want = (1 + p * f64(v)[0, 1]) / (1 + p)
     # of sums of up to 2: a weight to 1.5 units in its last place (3 EPS of values up to 2), three sums (2 EPS each), over 1.6; and the result's rounding
     within(f64(out), want, 8 * EPS + ROUND[BF16] * np.abs(want), "out")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,dim", [(1, 64), (7, 80), (40, 256), (200, 128), (20000, 64)])
+def test_attend_infinite_values(dtype, n, dim):
+    """A weight that is not zero times infinity is infinity, wherever the token is; infinities of both signs, or a value that is not a number,
+    give what is not a number; all else is as it was."""
+    rng = np.random.default_rng([50, n, dim])
+    c = make_cache(rng, [n, n], 1, dim, 16, dtype)
+    q = dev(rng.standard_normal((2, 3, dim)), dtype)
+    finite = attend64(c, q, [n, n], dim ** -0.5, 0.0)
+    want = finite[0].copy()
+    tab = c.table.cpu().numpy()
+    for d in range(40):                                 # (values 40 and above stay finite, and so does sequence 1)
+        kind, j = d % 5, int(rng.integers(n))
+        x = [math.inf, -math.inf, math.nan, math.inf, math.inf][kind]
+        c.v_pages[int(tab[0, j // 16]), 0, j % 16, d] = x
+        want[0, :, d] = x
+        if kind >= 3 and n > 1:                         # a second one: of the other sign, or the same
+            i = (j + 1 + int(rng.integers(n - 1))) % n
+            c.v_pages[int(tab[0, i // 16]), 0, i % 16, d] = -math.inf if kind == 3 else math.inf
+            want[0, :, d] = math.nan if kind == 3 else math.inf
+    out = f64(c.attend(q)[0])
+    assert np.array_equal(np.isnan(out), np.isnan(want)) and np.array_equal(np.isposinf(out), np.isposinf(want))
+    assert np.array_equal(np.isneginf(out), np.isneginf(want))
+    fine = np.isfinite(want)
+    within(out[fine], want[fine], finite[3][fine], "finite values")
