@@ -4,8 +4,8 @@
 // cached tokens j, and the weighted sum of the v_j.  Keys and values are read once, so memory bounds it: 4 * dim * heads operations for
 // 2 * dim * heads / group values (200 003 tokens of 8 key heads, 128 values in bfloat16: 131 us, 6.2 TB/s, where plain reads reach 7.2; 6.5 over
 // 32 x 8 192 tokens).  One pass: every wavefront takes tiles of consecutive tokens and keeps, for up to 16 query heads, the running maximum m,
-// the sum l of e^(s - m) and the sum o of e^(s - m) v; a tile with a larger maximum scales l and o by e^(m - m').  Parts of a sequence (wavefronts of
-// a workgroup, then workgroups) are joined the same way.
+// the sum l of e^(s - m) and the sum o of e^(s - m) v (times a power of two, see Tiles::bits); a tile with a larger maximum scales l and o by e^(m - m').
+// Parts of a sequence (wavefronts of a workgroup, then workgroups) are joined the same way.
 //
 // Layout.  S^T = K Q^T and O^T = V^T P^T on the matrix cores, 16 query heads as columns.  A lane's column is its query head (lane & 15) in both, so
 // that m and l live in the lane that needs them, and what S^T leaves in a lane -- the scores of tokens 4 * (lane >> 4) + r -- is
@@ -50,6 +50,9 @@ struct AttendArgs {
 // e^x for the difference x of two scores, which is exact or nearly so; scores times log2 e would be rounded at their own size.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
 
+// 2^e, e from -126 to 127.
+__device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
 // Two bfloat16 values, zero in the place of one that is not finite.
 __device__ __forceinline__ uint32_t finite_halves(uint32_t w)
 {
@@ -79,6 +82,10 @@ struct Tiles {
     __device__ int of(int len) const { return len > tokens ? (len + tokens - 1) / tokens : 1; }
     // workgroups that a pair of n tiles is worth: more than one where each has `enough`
     __device__ int worth(int n) const { return n < 2 * enough ? 1 : n / enough; }
+    // Sums of e^(s - m) v over a pair of n tiles are kept times 2^-bits, the number of its tokens at least twice: they are a part of a weighted mean
+    // then, and no larger than the values, where they could pass float32's range.  (What is lost is below 2^-126 * 2^bits: 1e-32 for
+    // 200 000 tokens.)
+    __device__ int bits(int n) const { return 33 - __builtin_clz(n) + (31 - __builtin_clz(tokens)); }
     __device__ void total(unsigned* tiles, unsigned* groups) const
     {
         const int lane = threadIdx.x & 63;
@@ -207,6 +214,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
     // A run is worked through a pair (sequence, head, block) at a time: those of its tiles that fall into one.
     struct Stretch {
         int seq, first, len, n, pair, from, to, h, row0, rows;        // first: tile of the sequence's first pair; n: tiles of a pair
+        float down;                                                   // 2^-bits
     };
     auto stretch = [&](int seq, int first) {
         Stretch x;
@@ -214,6 +222,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
         x.first = first;
         x.len = clamp_length(c.lengths[seq], c.capacity);
         x.n = tiles.of(x.len);
+        x.down = power(-tiles.bits(x.n));
         x.pair = (unsigned)(u - first) / (unsigned)x.n;
         x.from = u - first - x.pair * x.n;
         x.to = x.n - x.from < end - u ? x.n : x.from + (end - u);
@@ -283,7 +292,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
         }
     };
 
-    // row, values d and d + 1 of a pair's result: x and y over L
+    // row, values d and d + 1 of a pair's result: x and y over L, times 2^bits
     auto store_pair = [&](int seq, int head, int d, float x, float y) {
         if (d >= D) return;
         T* out = (T*)a.j.out.data + (long)seq * a.j.out.token + (long)head * a.j.out.head + d;
@@ -293,8 +302,8 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
         out[0] = e0;
         out[1] = e1;
     };
-    auto finish = [&](int seq, int head, int d, float M, float L, float x, float y) {
-        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    auto finish = [&](int seq, int head, int d, float M, float L, float up, float x, float y) {
+        const float inv = L == 0.0f ? 0.0f : up / L;
         store_pair(seq, head, d, x * inv, y * inv);
         if (d == 0) {
             const float z = L == 0.0f ? -__builtin_inff() : M + __builtin_amdgcn_logf(L) * LN2;
@@ -395,6 +404,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                 for (int r = 0; r < 4; ++r) {
                     p[s][r] = exp_of(sc[s][r] - m);
                     l += p[s][r];
+                    p[s][r] *= x.down;
                 }
             if constexpr (HALF) {
                 // P in three bfloat16 terms of 8 significant bits each, cut off and not rounded: they hold all of a float32's 24 bits, so that P is
@@ -473,7 +483,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
             // lane has o of query head l16, values (16 * p + 4 * quad + r) * PE + e: runs of 4 * PE values
             if (x.from == 0 && x.to == x.n && step == 1) {
                 const int head = x.h * a.group + x.row0 + l16;
-                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                const float inv = l == 0.0f ? 0.0f : power(tiles.bits(x.n)) / l;
                 if (l16 < x.rows) {
                     T* out = (T*)a.j.out.data + (long)x.seq * a.j.out.token + (long)head * a.j.out.head;
                     constexpr int E = 16 / (int)sizeof(T);
@@ -597,7 +607,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
             const int row = i / DP, d = i % DP;
             float M, L, y, z;
             join(x.slot, x.wave, x.parts, row, d, &M, &L, &y, &z);
-            if (whole) finish(x.seq, x.head0 + row, d, M, L, y, z);
+            if (whole) finish(x.seq, x.head0 + row, d, M, L, power(tiles.bits(x.n)), y, z);
             else {
                 put(to + 2 * ROWS + i, y, z);
                 if (d == 0) put(to + 2 * row, M, L);
@@ -648,7 +658,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
 #pragma unroll 1
             for (int p = lane; p < count; p += 64) L += exp_of(s_weight[row * count + p] - M) * s_sum[row * count + p];
             L = wave_sum(L);
-            const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+            const float inv = L == 0.0f ? 0.0f : power(tiles.bits(x.n)) / L;
 #pragma unroll 1
             for (int p = lane; p < count; p += 64) s_weight[row * count + p] = exp_of(s_weight[row * count + p] - M) * inv;
             if (lane == 0) {

@@ -869,3 +869,23 @@ def test_attend_infinite_values(dtype, n, dim):
     assert np.array_equal(np.isneginf(out), np.isneginf(want))
     fine = np.isfinite(want)
     within(out[fine], want[fine], finite[3][fine], "finite values")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [1, 2, 31, 64, 257, 30000])
+def test_attend_values_near_the_largest(dtype, n):
+    """A weighted mean is no larger than the largest value, however many tokens it is of."""
+    dim = 64
+    k = torch.zeros((1, n, dim), dtype=dtype, device="cuda")
+    k[0, :, 1] = torch.arange(n, device="cuda") % 2
+    v = torch.full((1, n, dim), 3e38, dtype=dtype, device="cuda")
+    v[..., dim // 2:] *= -1
+    q = torch.zeros((1, 4, dim), dtype=dtype, device="cuda")
+    q[0, 2:, 1] = 1.5                                   # heads with equal scores, and with two sizes of them
+    c = small_cache(k, v)
+    out, lse = c.attend(q, scale=1.0)
+    want = np.broadcast_to(f64(v)[0, 0], (1, 4, dim))
+    # weights of one size and their sum, in pieces: as in attend64, without an error of the scores
+    within(f64(out) / 1e38, want / 1e38, ((16 + 2 * math.sqrt(n)) * EPS + ROUND[dtype]) * np.abs(want) / 1e38, "out")
+    z = math.log(sum(math.exp(1.5 * (j % 2)) for j in range(n)))
+    within(f64(lse)[0, 2:], [z, z], (16 + abs(z)) * 4 * EPS, "lse")
