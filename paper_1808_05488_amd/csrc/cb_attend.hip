@@ -30,7 +30,7 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr float LOG2E = 1.44269504088896340736f, LOG2E_REST = (float)(1.44269504088896340736 - (double)LOG2E), LN2 = 0.69314718055994530942f;
 constexpr float LOWEST = -3.402823466e38f;       // of a maximum, so that nothing is subtracted from minus infinity
 constexpr int ROWS = ATTEND_ROWS;
 // Tiles of a wavefront that are worth a workgroup of their own: a part more costs its way through memory and the join.  (Five sequences of 1 - 9 001
@@ -47,8 +47,13 @@ struct AttendArgs {
     int pitch;                     // of a query head's scores
 };
 
-// e^x for the difference x of two scores, which is exact or nearly so; scores times log2 e would be rounded at their own size.
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
+// e^x for the difference x of two scores, which is exact or nearly so; scores times log2 e would be rounded at their own size.  What the product is
+// rounded by, and what log2 e is, come in as a factor 1 + rest: without it e^-80 would be off by 2e-6 of itself.
+__device__ __forceinline__ float exp_of(float x)
+{
+    const float y = x * LOG2E, rest = __builtin_fmaf(x, LOG2E_REST, __builtin_fmaf(x, LOG2E, -y)), e = __builtin_amdgcn_exp2f(y);
+    return e == 0.0f ? 0.0f : __builtin_fmaf(e, rest * LN2, e);      // (minus infinity leaves a rest that is not a number)
+}
 
 // 2^e, e from -126 to 127.
 __device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
@@ -306,7 +311,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
         const float inv = L == 0.0f ? 0.0f : up / L;
         store_pair(seq, head, d, x * inv, y * inv);
         if (d == 0) {
-            const float z = L == 0.0f ? -__builtin_inff() : M + __builtin_amdgcn_logf(L) * LN2;
+            const float z = L == 0.0f ? -__builtin_inff() : M + logf(L);
             if (a.j.lse) a.j.lse[(long)seq * a.j.q.heads + head] = z;
             a.lse[(long)seq * a.j.q.heads + head] = z;
         }
@@ -506,7 +511,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                             }
                         }
                     if (quad == 0) {
-                        const float z = l == 0.0f ? -__builtin_inff() : m + __builtin_amdgcn_logf(l) * LN2;
+                        const float z = l == 0.0f ? -__builtin_inff() : m + logf(l);
                         if (a.j.lse) a.j.lse[(long)x.seq * a.j.q.heads + head] = z;
                         a.lse[(long)x.seq * a.j.q.heads + head] = z;
                     }
@@ -662,7 +667,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
 #pragma unroll 1
             for (int p = lane; p < count; p += 64) s_weight[row * count + p] = exp_of(s_weight[row * count + p] - M) * inv;
             if (lane == 0) {
-                const float z = L == 0.0f ? -__builtin_inff() : M + __builtin_amdgcn_logf(L) * LN2;
+                const float z = L == 0.0f ? -__builtin_inff() : M + logf(L);
                 const long at = (long)x.seq * a.j.q.heads + x.head0 + row;
                 if (a.j.lse) a.j.lse[at] = z;
                 a.lse[at] = z;

@@ -889,3 +889,24 @@ def test_attend_values_near_the_largest(dtype, n):
     within(f64(out) / 1e38, want / 1e38, ((16 + 2 * math.sqrt(n)) * EPS + ROUND[dtype]) * np.abs(want) / 1e38, "out")
     z = math.log(sum(math.exp(1.5 * (j % 2)) for j in range(n)))
     within(f64(lse)[0, 2:], [z, z], (16 + abs(z)) * 4 * EPS, "lse")
+
+
+def test_attend_exponentials_are_exact_to_float32():
+    """One token of weight 1 and value 0, one of weight e^x and value 1: what comes out is e^x / (1 + e^x)."""
+    dim, heads = 64, 512
+    k = torch.zeros((1, 2, dim), device="cuda")
+    k[0, 1, 0] = 1.0
+    v = torch.zeros((1, 2, dim), device="cuda")
+    v[0, 1] = 1.0
+    c = small_cache(k, v, weight=True)
+    q = torch.zeros((1, heads, dim), device="cuda")
+    q[0, :, 0] = -torch.from_numpy(np.random.default_rng(51).uniform(0.0, 80.0, heads).astype(np.float32)).cuda()
+    out, lse = c.attend(q, scale=1.0, accumulate=True)
+    x = f64(q)[0, :, 0]
+    want = np.exp(x) / (1 + np.exp(x))
+    # e^x to 1 unit in the last place (2 EPS) and its second term, the sum, the division and its factor
+    within(f64(out)[0, :, 0], want, 8 * EPS * want, "out")
+    within(f64(lse)[0], np.log1p(np.exp(x)), 4 * EPS, "lse")
+    # both tokens' weights over all heads: the same, and 512 sums
+    total = np.array([heads - want.sum(), want.sum()])
+    within(f64(c.weight)[0, 0, :2], total, (8 + 512) * EPS * total, "weight")
