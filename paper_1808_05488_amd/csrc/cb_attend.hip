@@ -43,7 +43,8 @@ struct AttendArgs {
     int group, blocks;             // query heads of a key head, blocks of ROWS of them
     int q_aligned, out_aligned;    // to 16 bytes
     int* counters;
-    float *parts, *lse, *scores;
+    float *parts, *scores;
+    float2* sums;                  // of (sequence, query head): the maximum of the scores, 1 / the sum of e^(s - maximum) (0: there is none)
     int pitch;                     // of a query head's scores
 };
 
@@ -297,6 +298,10 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
         }
     };
 
+    auto put_sums = [&](long at, float M, float L) {
+        if (a.j.lse) a.j.lse[at] = L == 0.0f ? -__builtin_inff() : M + logf(L);
+        if (a.scores) a.sums[at] = make_float2(M, L == 0.0f ? 0.0f : 1.0f / L);
+    };
     // row, values d and d + 1 of a pair's result: x and y over L, times 2^bits
     auto store_pair = [&](int seq, int head, int d, float x, float y) {
         if (d >= D) return;
@@ -310,11 +315,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
     auto finish = [&](int seq, int head, int d, float M, float L, float up, float x, float y) {
         const float inv = L == 0.0f ? 0.0f : up / L;
         store_pair(seq, head, d, x * inv, y * inv);
-        if (d == 0) {
-            const float z = L == 0.0f ? -__builtin_inff() : M + logf(L);
-            if (a.j.lse) a.j.lse[(long)seq * a.j.q.heads + head] = z;
-            a.lse[(long)seq * a.j.q.heads + head] = z;
-        }
+        if (d == 0) put_sums((long)seq * a.j.q.heads + head, M, L);
     };
 
     // The tiles in order, those of the run's pairs behind each other: while one is computed the next one comes, its keys while this one's
@@ -510,11 +511,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                                     for (int z = 0; z < E; ++z) out[d + z] = e[z];
                             }
                         }
-                    if (quad == 0) {
-                        const float z = l == 0.0f ? -__builtin_inff() : m + logf(l);
-                        if (a.j.lse) a.j.lse[(long)x.seq * a.j.q.heads + head] = z;
-                        a.lse[(long)x.seq * a.j.q.heads + head] = z;
-                    }
+                    if (quad == 0) put_sums((long)x.seq * a.j.q.heads + head, m, l);
                 }
             } else {
                 const int slot = 2 * wave + (x.from == 0 && (step == 1 || wave == 0) ? 1 : 0);
@@ -666,12 +663,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
             const float inv = L == 0.0f ? 0.0f : power(tiles.bits(x.n)) / L;
 #pragma unroll 1
             for (int p = lane; p < count; p += 64) s_weight[row * count + p] = exp_of(s_weight[row * count + p] - M) * inv;
-            if (lane == 0) {
-                const float z = L == 0.0f ? -__builtin_inff() : M + logf(L);
-                const long at = (long)x.seq * a.j.q.heads + x.head0 + row;
-                if (a.j.lse) a.j.lse[at] = z;
-                a.lse[at] = z;
-            }
+            if (lane == 0) put_sums((long)x.seq * a.j.q.heads + x.head0 + row, M, L);
         }
         __syncthreads();
         // the sum over the parts, two values a thread: a team of threads for all of them takes every teams-th part, in order
@@ -713,7 +705,8 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
     }
 }
 
-// weight = decay * weight + the sum over the query heads of a key head of e^(s - lse), four slots a thread.  A launch of its own, since lse is
+// weight = decay * weight + the sum over the query heads of a key head of e^(s - m) / l, four slots a thread.  (Not e^(s - lse): the logarithm of l
+// would be rounded at the size of m, and be lost altogether beside a large one.)  A launch of its own, since m and l are
 // only known when all parts are joined: the scores wait in the scratch buffer (4 bytes a query head where keys and values are 4 * dim;
 // 24 sequences of 51 000 tokens in all, 32 query heads: 5 us here, 10 us of the 57 with the scores' way and the launch).
 __global__ __launch_bounds__(256) void weight_kernel(const AttendArgs a)
@@ -725,11 +718,10 @@ __global__ __launch_bounds__(256) void weight_kernel(const AttendArgs a)
     float* to = a.c.weight + ((long)seq * a.c.heads + h) * a.c.capacity + slot;
     f32x4 sum = f32x4{0, 0, 0, 0}, w = *reinterpret_cast<const f32x4*>(to);
     for (int g = 0; g < a.group; ++g) {
-        const float z = a.lse[q_head + g];
+        const float2 ml = a.sums[q_head + g];
         const f32x4 x = *reinterpret_cast<const f32x4*>(s + (long)g * a.pitch);
-        if (z != -__builtin_inff())
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] += exp_of(x[i] - z);
+        for (int i = 0; i < 4; ++i) sum[i] += exp_of(x[i] - ml.x) * ml.y;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = slot + i < len ? w[i] * a.j.decay + sum[i] : w[i];
@@ -756,7 +748,7 @@ hipError_t launch_attend(const AttendJob& j, const Cache& c, hipStream_t st)
     a.q_aligned = (uintptr_t)j.q.data % 16 == 0 && j.q.token % align == 0 && j.q.head % align == 0;
     a.counters = reinterpret_cast<int*>(c.scratch) + ATTEND_COUNTERS;
     a.parts = reinterpret_cast<float*>(c.scratch + plan.parts);
-    a.lse = reinterpret_cast<float*>(c.scratch + plan.lse);
+    a.sums = reinterpret_cast<float2*>(c.scratch + plan.sums);
     a.scores = j.accumulate ? reinterpret_cast<float*>(c.scratch + plan.scores) : nullptr;
     a.pitch = c.capacity;
     const int dp = c.dim <= 64 ? 64 : (c.dim <= 128 ? 128 : 256);

@@ -37,7 +37,7 @@ constexpr int ATTEND_COUNTERS = 64;
 constexpr int COUNTER_BYTES = (ATTEND_COUNTERS + MAX_GROUPS) * 4;
 
 struct ScratchPlan {
-    size_t parts, lse, scores, moves, total;
+    size_t parts, sums, scores, moves, total;
 };
 ScratchPlan scratch_plan(const Cache& c, int q_heads);
 

@@ -31,8 +31,8 @@ ScratchPlan scratch_plan(const Cache& c, int q_heads)
     const int dp = c.dim <= 64 ? 64 : (c.dim <= 128 ? 128 : 256);
     ScratchPlan p;
     p.parts = p.moves = align256(COUNTER_BYTES);
-    p.lse = p.parts + (q_heads ? align256((size_t)2 * MAX_GROUPS * ATTEND_ROWS * (dp + 2) * 4) : 0);
-    p.scores = p.lse + align256((size_t)c.seqs * q_heads * 4);
+    p.sums = p.parts + (q_heads ? align256((size_t)2 * MAX_GROUPS * ATTEND_ROWS * (dp + 2) * 4) : 0);
+    p.scores = p.sums + (c.weight ? align256((size_t)c.seqs * q_heads * 8) : 0);
     const size_t attend = p.scores + (c.weight ? align256((size_t)c.seqs * q_heads * c.capacity * 4) : 0);
     const size_t evict = p.moves + (c.weight ? align256(pairs * (1 + 2 * (size_t)c.capacity) * 4) : 0);
     p.total = attend > evict ? attend : evict;

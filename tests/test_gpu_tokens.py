@@ -910,3 +910,47 @@ def test_attend_exponentials_are_exact_to_float32():
     # both tokens' weights over all heads: the same, and 512 sums
     total = np.array([heads - want.sum(), want.sum()])
     within(f64(c.weight)[0, 0, :2], total, (8 + 512) * EPS * total, "weight")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [3, 200, 5000])
+@pytest.mark.parametrize("score", [0.0, 1e3, -1e4, 1e5, 1e6, -1e8, 3e38, -3e38])
+def test_weights_that_are_added_up_are_those_of_the_softmax(dtype, n, score):
+    """Every head's weights add up to one, however large the scores are that they come from."""
+    dim, group = 32, 3
+    k = torch.zeros((1, n, dim), dtype=dtype, device="cuda")
+    k[..., 3] = score
+    v = torch.randn((1, n, dim), device="cuda").to(dtype)
+    c = small_cache(k, v, weight=True)
+    q = torch.zeros((1, group, dim), dtype=dtype, device="cuda")
+    q[..., 3] = 1.0
+    c.attend(q, scale=1.0, accumulate=True)
+    got = f64(c.weight)[0, 0]
+    # equal scores: e^0 over a sum of n ones (exact below 2^24), a division, a product, a sum over the heads
+    within(got[:n], np.full(n, group / n), 8 * EPS * group / n, "weights")
+    assert not got[n:].any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_weights_of_scores_far_apart(dtype):
+    """Growing scores, scores of the lowest values, and small steps between large scores."""
+    n, dim = 200, 64
+    k = torch.zeros((3, n, dim), dtype=dtype, device="cuda")
+    k[0, :, 0] = torch.arange(n, device="cuda")
+    k[1, :, 0] = -3e38 if dtype == F32 else -2e38
+    k[2, :, 0] = torch.arange(n, device="cuda") % 2
+    k[2, :, 1] = 100000.0 if dtype == F32 else 99840.0
+    v = torch.randn((3, n, dim), device="cuda").to(dtype)
+    c = small_cache(k, v, weight=True)
+    q = torch.zeros((3, 4, dim), dtype=dtype, device="cuda")
+    q[:2, :, 0] = 1.0
+    q[2, :, :2] = 1.0
+    check_attend(c, q, [n] * 3, scale=1.0)
+    c.weight.zero_()
+    c.attend(q, scale=1.0, accumulate=True)
+    scores = f64(k)[:, :, :2] @ np.ones(2)
+    scores[:2] = f64(k)[:2, :, 0]
+    p = np.exp(scores - scores.max(1, keepdims=True))
+    want = 4 * p / p.sum(1, keepdims=True)
+    # exact scores and differences: e^x of up to -100 in two terms, a sum, a division, products
+    within(f64(c.weight)[:, 0, :n], want, (16 + 2 * math.sqrt(n)) * EPS * want + 1e-37, "weights")
