@@ -428,7 +428,8 @@ int cb_rotate(const cb_rotary *rotary, int32_t dtype, int64_t n_tokens, const in
  * max_pages * page_tokens is the most.  All arrays belong to the caller, who fills the table (entries behind a sequence's
  * last page are not read) and may change it between calls; a page that is written to belongs to one sequence.  What the
  * host cannot check is checked on the device: lengths are taken as 0 .. capacity, and slots whose page number is
- * not 0 .. n_pages - 1 hold no token: no page is written or read for them. */
+ * not 0 .. n_pages - 1 hold no token: no page is written or read for them, and attention leaves their weight as it is.  (Appending
+ * and eviction see to weight and time by slot numbers alone, such slots' too.) */
 typedef struct {
     int32_t n_seq, n_kv_heads;        /* n_seq 1 .. 65535, n_kv_heads 1 .. 1024 */
     int32_t head_dim;                 /* a multiple of 8 up to 256 */

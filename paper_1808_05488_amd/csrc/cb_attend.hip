@@ -713,6 +713,7 @@ __global__ __launch_bounds__(256) void weight_kernel(const AttendArgs a)
 {
     const int seq = blockIdx.z, h = blockIdx.y, slot = (blockIdx.x * 256 + threadIdx.x) * 4, len = clamp_length(a.c.lengths[seq], a.c.capacity);
     if (slot >= len) return;
+    if ((unsigned)a.c.table[(long)seq * a.c.max_pages + (slot >> a.c.page_shift)] >= (unsigned)a.c.n_pages) return;      // no page: no token
     const long q_head = (long)seq * a.j.q.heads + h * a.group;
     const float* s = a.scores + q_head * a.pitch + slot;
     float* to = a.c.weight + ((long)seq * a.c.heads + h) * a.c.capacity + slot;

@@ -954,3 +954,22 @@ def test_weights_of_scores_far_apart(dtype):
     want = 4 * p / p.sum(1, keepdims=True)
     # exact scores and differences: e^x of up to -100 in two terms, a sum, a division, products
     within(f64(c.weight)[:, 0, :n], want, (16 + 2 * math.sqrt(n)) * EPS * want + 1e-37, "weights")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_weights_of_slots_without_a_page_do_not_fade(dtype):
+    """They hold no token: their weight is left alone, whatever the page number is that is none."""
+    rng = np.random.default_rng(52)
+    lengths = [100, 33, 16]
+    c = make_cache(rng, lengths, 2, 64, 16, dtype)
+    dead = [(0, 2), (0, 6), (1, 0), (2, 0)]
+    q = dev(rng.standard_normal((3, 2, 64)), dtype)
+    want = attend64(c, q, lengths, 0.125, 0.0, 0.5, set(dead))
+    for (s, p), value in zip(dead, (-1, c.k_pages.shape[0], -2**31, 2**31 - 1)):
+        c.table[s, p] = value
+        want[2][s, :, p * 16:p * 16 + 16] = f64(c.weight)[s, :, p * 16:p * 16 + 16]
+    before = c.weight.clone()
+    c.attend(q, accumulate=True, decay=0.5)
+    within(f64(c.weight), want[2], want[5], "weight")
+    for s, p in dead:
+        assert torch.equal(c.weight[s, :, p * 16:p * 16 + 16], before[s, :, p * 16:p * 16 + 16])
