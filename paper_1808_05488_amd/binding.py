@@ -659,7 +659,6 @@ class Rotary:
         self.head_dim, self.n_axes = head_dim, len(pairs)
         self.plan = cb_rotary()
         _check(lib().cb_rotary_init(C.byref(d), C.byref(self.plan)), "cb_rotary_init")
-        self._address = C.addressof(self.plan)
 
     def rotate(self, q: torch.Tensor, positions: torch.Tensor, k: Optional[torch.Tensor] = None, inverse: bool = False,
                q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
@@ -680,7 +679,7 @@ class Rotary:
                 d = _fresh(k_out, dim)
             else:
                 d = _heads(k_out, "k_out", dtype, index, dim, k.shape[1], n)
-        status = lib().cb_rotate(self._address, _CB_DT[dtype], n, _dense(positions, "positions", torch.int32, index, (n, self.n_axes)),
+        status = lib().cb_rotate(C.byref(self.plan), _CB_DT[dtype], n, _dense(positions, "positions", torch.int32, index, (n, self.n_axes)),
                                  a, b, c, d, 1 if inverse else 0, _raw_stream(index))
         if status:
             _check(status, "cb_rotate")
@@ -771,7 +770,7 @@ class TokenCache:
             else:
                 d = _heads(q_out, "q_out", dtype, i, dim, q.shape[1], n)
         status = lib().cb_cache_append(
-            self._address, None if rotary is None else rotary._address, n if n < 2 ** 31 else -1,
+            self._address, None if rotary is None else C.byref(rotary.plan), n if n < 2 ** 31 else -1,
             _dense(positions, "positions", torch.int32, i, (n, 1 if rotary is None else rotary.n_axes)),
             _dense(offsets, "offsets", torch.int32, i, (self.n_seq + 1,)), _dense(start, "start", torch.int32, i, (self.n_seq,)),
             a, b, c, d, _raw_stream(i))

@@ -1,7 +1,9 @@
 """The token operators on the GPU against plain implementations in 64 bits on the host: rotary positions, appending to the paged
 cache, attention of one token over it, eviction; what goes wrong at edges (empty sequences, pages that end inside a tile, slots
 without a page, garbage behind the last token), strides, streams, graphs, and pages beyond 4 GB."""
+import copy
 import math
+import pickle
 
 import numpy as np
 import pytest
@@ -973,3 +975,22 @@ def test_weights_of_slots_without_a_page_do_not_fade(dtype):
     within(f64(c.weight), want[2], want[5], "weight")
     for s, p in dead:
         assert torch.equal(c.weight[s, :, p * 16:p * 16 + 16], before[s, :, p * 16:p * 16 + 16])
+
+
+def test_copies_of_a_rotary():
+    """A copy goes by its own frequencies, whatever becomes of the first one."""
+    rng = np.random.default_rng(53)
+    q, pos = dev(rng.standard_normal((9, 2, 64)), F32), dev(rng.integers(0, 500, (9, 3)).astype(np.int32))
+    first = cb.Rotary(64, (8, 12, 12))
+    want = first.rotate(q, pos)
+    others = [copy.deepcopy(first), pickle.loads(pickle.dumps(first))]
+    for r in others:
+        assert torch.equal(r.rotate(q, pos), want)
+    first.plan.desc.pairs[0] = 99                       # is refused from here on
+    with pytest.raises(cb.CBError):
+        first.rotate(q, pos)
+    c = cb.TokenCache.create(9, 2, 64, 16, F32, 16)
+    for r in others:
+        assert torch.equal(r.rotate(q, pos), want)
+        c.append(q, q, pos, rotary=r, start=torch.zeros(9, dtype=torch.int32, device="cuda"))
+        assert torch.equal(c.k_pages[:, :, 0], want)
