@@ -719,6 +719,10 @@ class TokenCache:
         self._lse = {}                     # by query heads: what an lse is like
         self._scratch(0, scratch)
 
+    def __reduce_ex__(self, protocol):
+        # (copy, deepcopy and pickle come here; the structure would be shared, or hold addresses of another process)
+        raise TypeError("a TokenCache is not copied: make another one of tensors, or of copies of them")
+
     @classmethod
     def create(cls, n_seq: int, n_kv_heads: int, head_dim: int, capacity: int, dtype=torch.bfloat16, page_tokens: int = 64,
                device="cuda", evictable: bool = True):

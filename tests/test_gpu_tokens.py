@@ -994,3 +994,11 @@ def test_copies_of_a_rotary():
         assert torch.equal(r.rotate(q, pos), want)
         c.append(q, q, pos, rotary=r, start=torch.zeros(9, dtype=torch.int32, device="cuda"))
         assert torch.equal(c.k_pages[:, :, 0], want)
+
+
+def test_a_cache_is_not_copied():
+    """Neither object could know of a scratch buffer that the other one makes or lets go."""
+    c = cb.TokenCache.create(2, 2, 32, 64, F32, 16)
+    for made in (copy.copy, copy.deepcopy, pickle.dumps):
+        with pytest.raises(TypeError, match="not copied"):
+            made(c)
