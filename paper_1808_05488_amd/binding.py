@@ -646,6 +646,27 @@ def _dense(t: Optional[torch.Tensor], what: str, dtype, index: int, shape) -> Op
     return t.data_ptr()
 
 
+class _Rotation(torch.autograd.Function):
+    """Rotary.rotate in a graph: the gradient of a rotation is the rotation back."""
+
+    @staticmethod
+    def forward(ctx, rotary, inverse, positions, q, k):
+        ctx.rotary, ctx.inverse = rotary, inverse
+        ctx.save_for_backward(positions)
+        ctx.set_materialize_grads(False)
+        out = rotary.rotate(q, positions, k, inverse)
+        q_out, k_out = (out, None) if k is None else out
+        ctx.mark_non_differentiable(*(y for x, y in ((q, q_out), (k, k_out)) if x is not None and not x.requires_grad))
+        return q_out, k_out
+
+    @staticmethod
+    def backward(ctx, *grads):
+        positions, = ctx.saved_tensors
+        # (a gradient comes in any strides: a sum's is one value, repeated)
+        back = [None if g is None else ctx.rotary.rotate(g.contiguous(), positions, inverse=not ctx.inverse) for g in grads]
+        return None, None, None, back[0], back[1]
+
+
 class Rotary:
     """Rotary positions with several axes: pairs[a] pairs of a head turn with a token's position on axis a."""
 
@@ -663,7 +684,13 @@ class Rotary:
     def rotate(self, q: torch.Tensor, positions: torch.Tensor, k: Optional[torch.Tensor] = None, inverse: bool = False,
                q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
         """q (tokens x heads x head_dim) turned by positions (tokens x axes, int32), and k with it: q_out, or (q_out, k_out).
-        inverse: turned back, which is also the gradient of q from that of q_out.  An output may be its input."""
+        inverse: turned back, which is also the gradient of q from that of q_out: q and k may be parts of a graph, if their outputs are not
+        given.  An output may be its input."""
+        if (q.requires_grad or (k is not None and k.requires_grad)) and torch.is_grad_enabled():
+            if q_out is not None or k_out is not None:
+                raise AssertionError("outputs that are given carry no gradient: rotate without them, or under torch.no_grad()")
+            q_out, k_out = _Rotation.apply(self, inverse, positions, q, k)
+            return q_out if k is None else (q_out, k_out)
         n, dtype, index, dim = q.shape[0], q.dtype, q.get_device(), self.head_dim
         assert index >= 0 and dtype in _CB_DT, f"q: {dtype} on {q.device}"
         a, c, d = _heads(q, "q", dtype, index, dim), None, None

@@ -1002,3 +1002,56 @@ def test_a_cache_is_not_copied():
     for made in (copy.copy, copy.deepcopy, pickle.dumps):
         with pytest.raises(TypeError, match="not copied"):
             made(c)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_gradients_go_through_the_rotation(dtype, layout, inverse):
+    rng = np.random.default_rng([54, layout])
+    n, dim, pairs = 21, 40, (5, 6, 6)
+    pos = dev(rng.integers(0, 300, (n, 3)).astype(np.int32))
+    rot = cb.Rotary(dim, pairs, layout=layout)
+    qkv = dev(rng.standard_normal((n, 7, dim)), dtype)
+    gq, gk = dev(rng.standard_normal((n, 4, dim)), dtype), dev(rng.standard_normal((n, 2, dim)), dtype)
+    want = rot.rotate(qkv[:, :4], pos, k=qkv[:, 4:6], inverse=inverse)
+    back = rot.rotate(gq, pos, k=gk, inverse=not inverse)
+    x = qkv.clone().requires_grad_()
+    out = rot.rotate(x[:, :4], pos, k=x[:, 4:6], inverse=inverse)
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+    torch.autograd.backward(out, (gq, gk))
+    assert torch.equal(x.grad[:, :4], back[0]) and torch.equal(x.grad[:, 4:6], back[1]) and not bool(x.grad[:, 6:].any())
+    # q alone, and k alone of both; gradients of any strides (a sum's are one value, repeated)
+    x.grad = None
+    rot.rotate(x[:, :4], pos, inverse=inverse).sum().backward()
+    ones = torch.ones_like(gq)
+    assert torch.equal(x.grad[:, :4], rot.rotate(ones, pos, inverse=not inverse)) and not bool(x.grad[:, 4:].any())
+    x.grad = None
+    q, k = rot.rotate(qkv[:, :4], pos, k=x[:, 4:6], inverse=inverse)
+    assert not q.requires_grad
+    k.backward(gk.transpose(1, 2).contiguous().transpose(1, 2))
+    assert torch.equal(x.grad[:, 4:6], back[1]) and not bool(x.grad[:, :4].any())
+    # one of two results is used
+    x.grad = None
+    rot.rotate(x[:, :4], pos, k=x[:, 4:6], inverse=inverse)[0].backward(gq)
+    assert torch.equal(x.grad[:, :4], back[0]) and not bool(x.grad[:, 4:].any())
+    # outputs that are given are written outside of autograd's sight
+    for kw in (dict(q_out=torch.empty_like(gq)), dict(k=gk, k_out=torch.empty_like(gk))):
+        with pytest.raises(AssertionError, match="gradient"):
+            rot.rotate(x[:, :4], pos, **kw)
+    with torch.no_grad():
+        got = torch.empty_like(gq)
+        assert torch.equal(rot.rotate(x[:, :4], pos, inverse=inverse, q_out=got), want[0]) and not got.requires_grad
+
+
+def test_gradient_of_the_gradient_of_the_rotation():
+    """Linear in q: what a loss of the gradient gives back is the rotation itself."""
+    rng = np.random.default_rng(55)
+    pos = dev(rng.integers(0, 300, (5, 2)).astype(np.int32))
+    rot = cb.Rotary(16, (3, 4))
+    x, g, u = (dev(rng.standard_normal((5, 2, 16)), F32) for _ in range(3))
+    x.requires_grad_()
+    g.requires_grad_()
+    grad, = torch.autograd.grad(rot.rotate(x, pos), x, g, create_graph=True)
+    again, = torch.autograd.grad(grad, g, u)
+    assert torch.equal(again, rot.rotate(u, pos))
