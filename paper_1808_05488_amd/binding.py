@@ -646,6 +646,11 @@ def _dense(t: Optional[torch.Tensor], what: str, dtype, index: int, shape) -> Op
     return t.data_ptr()
 
 
+def _refuse_grad(where: str) -> None:
+    if torch.is_grad_enabled():
+        raise AssertionError(f"{where} carries no gradient: give it detached tensors, or call it under torch.no_grad()")
+
+
 class _Rotation(torch.autograd.Function):
     """Rotary.rotate in a graph: the gradient of a rotation is the rotation back."""
 
@@ -788,7 +793,10 @@ class TokenCache:
                q: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None, start: Optional[torch.Tensor] = None,
                q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """Rows offsets[s] .. offsets[s + 1] - 1 of k and v (without offsets row s) behind the tokens of sequence s, or from
-        slot start[s] on; keys rotated if there is a rotary, and q (row for row), which is returned."""
+        slot start[s] on; keys rotated if there is a rotary, and q (row for row), which is returned (rows behind the last
+        sequence's are not written).  Tensors that want a gradient are refused."""
+        if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad):
+            _refuse_grad("append")
         n, dtype, i, dim = k.shape[0], self.dtype, self._index, self.head_dim
         a = _heads(k, "k", dtype, i, dim, self.n_kv_heads)
         b = _heads(v, "v", dtype, i, dim, self.n_kv_heads, n)
@@ -812,7 +820,9 @@ class TokenCache:
     def attend(self, q: torch.Tensor, scale: Optional[float] = None, softcap: float = 0.0, accumulate: bool = False,
                decay: float = 1.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
         """(out, lse) of one query token per sequence (q: sequences x query heads x head_dim).  scale: 1 / sqrt(head_dim) if not
-        given.  accumulate: the cache's weight becomes decay * weight + the weights of this call."""
+        given.  accumulate: the cache's weight becomes decay * weight + the weights of this call.  A q that wants a gradient is refused."""
+        if q.requires_grad:
+            _refuse_grad("attend")
         dtype, i, dim = self.dtype, self._index, self.head_dim
         a = _heads(q, "q", dtype, i, dim, None, self.n_seq)
         heads = q.shape[1]

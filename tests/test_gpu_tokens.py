@@ -1055,3 +1055,23 @@ def test_gradient_of_the_gradient_of_the_rotation():
     grad, = torch.autograd.grad(rot.rotate(x, pos), x, g, create_graph=True)
     again, = torch.autograd.grad(grad, g, u)
     assert torch.equal(again, rot.rotate(u, pos))
+
+
+def test_the_cache_refuses_what_wants_a_gradient():
+    """What is cached, and what is read from it, carries none: a graph that would end there without a word is refused."""
+    c = cb.TokenCache.create(2, 2, 32, 64, F32, 16)
+    k, v, q = torch.randn((2, 2, 32), device="cuda"), torch.randn((2, 2, 32), device="cuda"), torch.randn((2, 4, 32), device="cuda")
+    pos, rot = torch.zeros((2, 1), dtype=torch.int32, device="cuda"), cb.Rotary(32, (16,))
+    wants = lambda x: x.clone().requires_grad_()  # noqa: E731
+    for args, kw in (((wants(k), v), {}), ((k, wants(v)), {}), ((k, v, pos, rot), dict(q=wants(q)))):
+        with pytest.raises(AssertionError, match="gradient"):
+            c.append(*args, **kw)
+    assert not bool(c.lengths.any())
+    with pytest.raises(AssertionError, match="gradient"):
+        c.attend(wants(q))
+    with torch.no_grad():
+        c.append(wants(k), wants(v), pos, rot, q=wants(q))
+        c.attend(wants(q))
+    assert c.lengths.tolist() == [1, 1]
+    c.append(wants(k).detach(), v)
+    assert c.lengths.tolist() == [2, 2]
