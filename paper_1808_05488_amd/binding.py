@@ -390,7 +390,12 @@ class Layer:
         self.C, self.H, self.W = Cc, h_in, w_in
         self.O, self.Ho, self.Wo = cb_layer_out_shape(self.handle)
         self._keep = (weight, bias)
+        self._producers = []               # layers whose list this one may have taken over
         self._views = _Views(self.state_buf, _TORCH_DT[self.dtype])
+
+    def _fed_by(self, producer):
+        if isinstance(producer, Layer) and producer not in self._producers:
+            self._producers.append(producer)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -424,6 +429,7 @@ class Layer:
         if isinstance(producer, Pool):
             p = cb_process_frame_propagated(self.handle, x, None, producer.handle)
         else:
+            self._fed_by(producer)
             p = cb_process_frame_propagated(self.handle, x, producer.handle, None)
         return self._views(p, (self.O, self.Ho, self.Wo))
 
@@ -444,11 +450,20 @@ class Layer:
         return m_t, mt_t, idx.astype(np.int32), n
 
     def listed(self):
-        """(list, count) of the last frame's changed output pixels as views of the layer's own memory: Ho * Wo int32 linear indices, of which the
-        first count[0] are the last frame's, in ascending order.  Nothing waits; the next frame overwrites both."""
+        """(list, count) of the last frame's changed output pixels as views of the memory of the layer that made them (a propagated 1 x 1 layer takes its
+        producer's): Ho * Wo int32 linear indices, of which the first count[0] are the last frame's, in ascending order.  Nothing waits; that
+        layer's next frame overwrites both."""
         idx, cnt = C.c_void_p(), C.c_void_p()
         _check(lib().cb_layer_changes(self.handle, None, None, C.byref(idx), C.byref(cnt)), "cb_layer_changes")
-        return (_view(self.state_buf, idx.value, (self.Ho * self.Wo,), torch.int32), _view(self.state_buf, cnt.value, (1,), torch.int32))
+        made, seen = [self], {id(self)}
+        for layer in made:                 # (grows as it goes)
+            if layer.state_buf.data_ptr() <= idx.value < layer.state_buf.data_ptr() + layer.state_buf.numel():
+                return (_view(layer.state_buf, idx.value, (self.Ho * self.Wo,), torch.int32), _view(layer.state_buf, cnt.value, (1,), torch.int32))
+            for p in layer._producers:
+                if id(p) not in seen:
+                    seen.add(id(p))
+                    made.append(p)
+        raise RuntimeError("the list is that of a layer that this object has not been given as a producer")
 
     def state(self) -> torch.Tensor:
         return self._views(cb_layer_state(self.handle), (self.C, self.H, self.W))
@@ -540,6 +555,9 @@ class Network:
             self.stages[s].pool = self.pools[s].handle if self.pools[s] is not None else None
         last = self.pools[-1] if self.pools[-1] is not None else self.layers[-1]
         self.out_shape = (last.O, last.Hp, last.Wp) if self.pools[-1] is not None else (last.O, last.Ho, last.Wo)
+        for a, p, b in zip(self.layers, self.pools, self.layers[1:]):
+            if p is None:
+                b._fed_by(a)
         self._views = last._views
         self.dtype = self.layers[-1].dtype
         self.device = self.layers[0].device

@@ -1075,3 +1075,36 @@ def test_the_cache_refuses_what_wants_a_gradient():
     assert c.lengths.tolist() == [1, 1]
     c.append(wants(k).detach(), v)
     assert c.lengths.tolist() == [2, 2]
+
+
+@pytest.mark.parametrize("network", [True, False])
+def test_lists_of_layers_that_take_them_over(network):
+    """A propagated 1 x 1 layer's list is its producer's, which may have taken it over itself; behind a pooling stage it is the layer's own."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    rand = lambda *shape: torch.randn(shape, generator=g, device="cuda")  # noqa: E731
+    h, w = 20, 28
+    layers = [cb.Layer(rand(8, 3, 3, 3), None, 1, 1, h, w, True)]
+    layers += [cb.Layer(rand(8, 8, 1, 1), None, 1, 0, h, w, True, mode=cb.CB_PROPAGATE) for _ in range(2)]
+    pools = [None, None, cb.Pool(layers[-1], 2)]
+    layers.append(cb.Layer(rand(4, 8, 1, 1), None, 1, 0, h // 2, w // 2, True, mode=cb.CB_PROPAGATE))
+    pools.append(None)
+    net = cb.Network(layers, pools)
+    image = rand(3, h, w)
+    for frame in range(3):
+        if frame:
+            image = image.clone()
+            image[:, 3 + frame:6, 4:9] += 1.0
+        if network:
+            net.forward(image, [0.01] * 4)
+        else:
+            x = layers[0].process_frame(image, 0.01)
+            for i in (1, 2):
+                x = layers[i].process_frame_propagated(x, layers[i - 1])
+            layers[3].process_frame_propagated(pools[2].process(), pools[2])
+        for layer in layers:
+            want = layer.changes_host()
+            pixel, count = layer.listed()
+            assert pixel.shape == (layer.Ho * layer.Wo,) and int(count) == want[3] > 0
+            assert np.array_equal(pixel[:int(count)].cpu().numpy(), want[2])
+        assert layers[2].listed()[0].data_ptr() == layers[0].listed()[0].data_ptr() or frame == 0
