@@ -626,6 +626,7 @@ class Pool:
 
 
 # ---------------------------------------------------------------- tokens of a stream
+# (What keeps addresses of the wrong kind from the GPU is raised, not asserted: it holds under python -O too.)
 _CB_DT = {torch.float32: CB_F32, torch.bfloat16: CB_BF16}
 # The structures of one call, packed anew for it (a call may run while another thread packs its own).  A call's work on the host is
 # part of a small call's time: packing takes 0.2 us a structure, filling a ctypes one 0.5 us.
@@ -695,7 +696,8 @@ class Rotary:
 
     def __init__(self, head_dim: int, pairs, base: float = 10000.0, layout: int = CB_PAIRS_HALVES, ladder: int = CB_LADDER_SHARED):
         pairs = [int(n) for n in pairs]
-        assert len(pairs) <= CB_ROTARY_MAX_AXES
+        if len(pairs) > CB_ROTARY_MAX_AXES:
+            raise AssertionError(f"{len(pairs)} axes: {CB_ROTARY_MAX_AXES} at most")
         d = cb_rotary_desc()
         d.head_dim, d.n_axes, d.layout, d.ladder, d.base = head_dim, len(pairs), layout, ladder, base
         for a, n in enumerate(pairs):
@@ -715,7 +717,8 @@ class Rotary:
             q_out, k_out = _Rotation.apply(self, inverse, positions, q, k)
             return q_out if k is None else (q_out, k_out)
         n, dtype, index, dim = q.shape[0], q.dtype, q.get_device(), self.head_dim
-        assert index >= 0 and dtype in _CB_DT, f"q: {dtype} on {q.device}"
+        if index < 0 or dtype not in _CB_DT:
+            raise AssertionError(f"q: {dtype} on {q.device}; needed: float32 or bfloat16 on a GPU")
         a, c, d = _heads(q, "q", dtype, index, dim), None, None
         if q_out is None:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
@@ -747,7 +750,9 @@ class TokenCache:
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
                  weight: Optional[torch.Tensor] = None, time: Optional[torch.Tensor] = None,
                  scratch: Optional[torch.Tensor] = None):
-        assert k_pages.is_cuda and k_pages.dim() == 4 and k_pages.dtype in _CB_DT and table.dim() == 2
+        if not (k_pages.is_cuda and k_pages.dim() == 4 and k_pages.dtype in _CB_DT and table.dim() == 2):
+            raise AssertionError(f"k_pages: {k_pages.dtype} {tuple(k_pages.shape)} on {k_pages.device}, table: {tuple(table.shape)}; needed: float32 or "
+                                 f"bfloat16 (pages, key heads, page_tokens, head_dim) on a GPU, and (sequences, pages of a sequence)")
         n_pages, heads, page, dim = k_pages.shape
         self.n_seq, self.n_kv_heads, self.head_dim, self.capacity = table.shape[0], heads, dim, table.shape[1] * page
         self.device, self.dtype, self._index = k_pages.device, k_pages.dtype, k_pages.get_device()
@@ -797,13 +802,14 @@ class TokenCache:
             given = self.scratch
         if given is None:
             # its counters are cleared once, now: a recorded clearing would only come with the graph's first replay
-            assert not torch.cuda.is_current_stream_capturing(), \
-                f"a scratch buffer for {n_q_heads} query heads has to be made before a graph is recorded: attend once before, or give one"
+            if torch.cuda.is_current_stream_capturing():
+                raise AssertionError(f"a scratch buffer for {n_q_heads} query heads has to be made before a graph is recorded: attend once before, or give one")
             given = _alloc(nbytes, self.device)
             given.zero_()
             if self._room >= 0:
                 self._outgrown.append(self.scratch)
-        assert given.dtype == torch.uint8 and given.device == self.device and given.is_contiguous()
+        if not (given.dtype == torch.uint8 and given.device == self.device and given.is_contiguous()):
+            raise AssertionError(f"scratch: {given.dtype}, strides {given.stride()}, on {given.device}; needed: dense uint8 on {self.device}")
         self.scratch, self._room = given, n_q_heads
         self.desc.scratch_dev, self.desc.scratch_bytes = given.data_ptr(), given.numel()
 

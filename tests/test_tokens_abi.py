@@ -2,6 +2,10 @@
 up, and a call that would not refuse them is not made."""
 import ctypes as C
 import math
+import os
+import subprocess
+import sys
+import textwrap
 
 import pytest
 
@@ -190,3 +194,39 @@ def test_scratch_sizes():
         assert L.cb_cache_scratch_bytes(C.byref(cache()), bad, C.byref(n)) == cb.CB_EINVAL
     assert L.cb_cache_scratch_bytes(C.byref(cache()), 4, None) == cb.CB_EINVAL
     assert L.cb_cache_scratch_bytes(None, 4, C.byref(n)) == cb.CB_EINVAL
+
+
+def without_asserts(code):
+    """What python -O prints of the code (assert statements are gone there), with the error's type in place of one that is raised."""
+    text = "import torch\nimport paper_1808_05488_amd as cb\ntry:\n" + textwrap.indent(textwrap.dedent(code), "    ") + \
+           "\nexcept Exception as e:\n    print(type(e).__name__, e)\nelse:\n    print('done')\n"
+    r = subprocess.run([sys.executable, "-O", "-c", text], capture_output=True, text=True, timeout=300,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0, r.stderr
+    return r.stdout.strip()
+
+
+def test_addresses_of_the_host_are_refused_without_asserts():
+    got = without_asserts("""
+        x = lambda *shape, dtype=torch.float32: torch.zeros(shape, dtype=dtype)
+        cb.TokenCache(x(4, 2, 16, 32), x(4, 2, 16, 32), x(2, 2, dtype=torch.int32), x(2, dtype=torch.int32))""")
+    assert got.startswith("AssertionError") and "on a GPU" in got
+    got = without_asserts("""
+        cb.Rotary(32, (16,)).rotate(torch.zeros(0, 2, 32), torch.zeros((0, 1), dtype=torch.int32))""")
+    assert got.startswith("AssertionError") and "on a GPU" in got
+
+
+def test_what_a_scratch_buffer_has_to_be_is_checked_without_asserts():
+    # (a stand-in for a cache: nothing here has a GPU)
+    code = """
+        import types
+        from unittest import mock
+        me = types.SimpleNamespace(scratch_bytes=lambda n: 512, _room=-1, device=torch.device("cpu"), desc=types.SimpleNamespace())
+        with mock.patch.object(torch.cuda, "is_current_stream_capturing", return_value=%s):
+            cb.TokenCache._scratch(me, 4, %s)"""
+    got = without_asserts(code % (True, None))
+    assert got.startswith("AssertionError") and "attend once before" in got
+    for given in ("torch.zeros(512, dtype=torch.int32)", "torch.zeros(1024, dtype=torch.uint8)[::2]", "torch.zeros(512, dtype=torch.uint8, device='meta')"):
+        got = without_asserts(code % (False, given))
+        assert got.startswith("AssertionError") and "scratch" in got
+    assert without_asserts(code % (False, "torch.zeros(512, dtype=torch.uint8)")) == "done"
