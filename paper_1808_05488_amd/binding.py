@@ -716,6 +716,8 @@ class Rotary:
                 raise AssertionError("outputs that are given carry no gradient: rotate without them, or under torch.no_grad()")
             q_out, k_out = _Rotation.apply(self, inverse, positions, q, k)
             return q_out if k is None else (q_out, k_out)
+        if k is None and k_out is not None:
+            raise AssertionError("k_out without k")
         n, dtype, index, dim = q.shape[0], q.dtype, q.get_device(), self.head_dim
         if index < 0 or dtype not in _CB_DT:
             raise AssertionError(f"q: {dtype} on {q.device}; needed: float32 or bfloat16 on a GPU")
@@ -832,6 +834,8 @@ class TokenCache:
                 d = _fresh(q_out, dim)
             else:
                 d = _heads(q_out, "q_out", dtype, i, dim, q.shape[1], n)
+        elif q_out is not None:
+            raise AssertionError("q_out without q")
         status = lib().cb_cache_append(
             self._address, None if rotary is None else C.byref(rotary.plan), n if n < 2 ** 31 else -1,
             _dense(positions, "positions", torch.int32, i, (n, 1 if rotary is None else rotary.n_axes)),

@@ -1108,3 +1108,15 @@ def test_lists_of_layers_that_take_them_over(network):
             assert pixel.shape == (layer.Ho * layer.Wo,) and int(count) == want[3] > 0
             assert np.array_equal(pixel[:int(count)].cpu().numpy(), want[2])
         assert layers[2].listed()[0].data_ptr() == layers[0].listed()[0].data_ptr() or frame == 0
+
+
+def test_outputs_of_nothing_are_refused():
+    """An output without its input would come back unwritten."""
+    c = cb.TokenCache.create(2, 2, 32, 64, F32, 16)
+    k, out = torch.zeros((2, 2, 32), device="cuda"), torch.zeros((2, 4, 32), device="cuda")
+    pos, rot = torch.zeros((2, 1), dtype=torch.int32, device="cuda"), cb.Rotary(32, (16,))
+    with pytest.raises(AssertionError, match="q_out"):
+        c.append(k, k, pos, rot, q_out=out)
+    assert not bool(c.lengths.any())
+    with pytest.raises(AssertionError, match="k_out"):
+        rot.rotate(out, pos, k_out=k)
