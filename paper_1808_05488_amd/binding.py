@@ -745,7 +745,8 @@ class TokenCache:
     """A paged key-value cache (cb_cache) over tensors of the caller's, and its scratch buffer.
 
     k_pages, v_pages: pages x key heads x page_tokens x head_dim; table: sequences x pages of a sequence, int32; lengths:
-    sequences, int32; weight (float32) and time (int32): sequences x key heads x capacity, needed to evict.  Calls run on
+    sequences, int32; weight (float32) and time (int32): sequences x key heads x capacity, needed to evict.  scratch, if
+    it is given (caches may share one): dense uint8, 256-byte aligned, scratch_bytes(query heads) long, and zeroed before the first call.  Calls run on
     the current stream; calls that share a cache or a scratch buffer have to be on one stream, or ordered.  A graph that
     has recorded calls needs the object as long as it is replayed: its scratch buffers stay until then."""
 
