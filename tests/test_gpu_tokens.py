@@ -2,6 +2,7 @@
 cache, attention of one token over it, eviction; what goes wrong at edges (empty sequences, pages that end inside a tile, slots
 without a page, garbage behind the last token), strides, streams, graphs, and pages beyond 4 GB."""
 import copy
+import ctypes as C
 import math
 import pickle
 
@@ -1120,3 +1121,112 @@ def test_outputs_of_nothing_are_refused():
     assert not bool(c.lengths.any())
     with pytest.raises(AssertionError, match="k_out"):
         rot.rotate(out, pos, k_out=k)
+
+
+def class_cache(rng, lengths, heads, dim, page, dtype):
+    """Long sequences over 64 pages that are only read: the tables name them in no order, again and again.  A page is of one of 16 classes (another
+    one for each key head): query head i of 16 scores 0 at pages of class i and so little at others that their weight is zero; values
+    i, i + 16, ... of those pages are zero, and large on all others."""
+    cls = (np.arange(64)[:, None] + 5 * np.arange(heads)) % 16
+    k = np.where(np.arange(16) == cls[..., None], 0.0, -30000.0)
+    v = np.where(np.arange(dim) % 16 == cls[..., None], 0.0, 2.0 ** 20)
+    k = np.concatenate([k, np.zeros((64, heads, dim - 16))], 2)
+    pages = [dev(x.astype(np.float32)).to(dtype)[:, :, None].expand(-1, -1, page, -1).contiguous() for x in (k, v)]
+    table = rng.integers(0, 64, (len(lengths), -(-max(lengths) // page))).astype(np.int32)
+    c = cb.TokenCache(*pages, dev(table), dev(np.array(lengths, np.int32)))
+    q = torch.zeros((len(lengths), heads, 16, dim), dtype=dtype, device="cuda")
+    q[:, :, range(16), range(16)] = 1.0
+    counts = np.zeros((len(lengths), heads, 16))        # tokens of a class
+    for s, n in enumerate(lengths):
+        held = np.bincount(table[s], np.clip(n - page * np.arange(table.shape[1]), 0, page), 64)
+        for h in range(heads):
+            counts[s, h] = np.bincount(cls[:, h], held, 16)
+    return c, q.flatten(1, 2), counts
+
+
+@pytest.mark.parametrize("dtype,dim,page,lengths,heads", [
+    # a run within one pair (dealt to the wavefronts in turn): up to 137 tiles a wavefront on 256 compute units, page numbers come for 32 or 64 at a time
+    (BF16, 64, 32, [9_000_000], 1), (F32, 64, 32, [9_000_001], 1), (BF16, 256, 16, [1_400_000], 1), (F32, 128, 64, [2_500_017], 1),
+    (BF16, 64, 16, [1_500_000, 3, 0, 1_700_000, 40_000], 2), (F32, 256, 32, [70_000] * 16 + [1, 17], 1),
+    # more pairs than workgroups: runs over ends of heads and sequences
+    (BF16, 64, 64, [40_000, 1, 0, 37_001, 16, 45_000, 39_999] + [20_000] * 6, 96), (F32, 64, 16, [40_000, 1, 0, 37_001, 16] + [20_000] * 8, 48),
+    (BF16, 128, 32, [40_000, 1, 0, 37_001, 16] + [20_000] * 8, 48), (F32, 256, 64, [40_000, 1, 0, 37_001, 16] + [20_000] * 8, 24)])
+def test_attend_wavefronts_with_more_tiles_than_page_numbers(dtype, dim, page, lengths, heads):
+    rng = np.random.default_rng([56, dim, len(lengths)])
+    c, q, counts = class_cache(rng, lengths, heads, dim, page, dtype)
+    out, lse = c.attend(q, scale=1.0)
+    out = f64(out).reshape(counts.shape + (dim,))
+    own = np.arange(dim) % 16 == np.arange(16)[:, None]
+    some = counts > 0
+    # a wrong page among the values: 2^20 / n at least
+    assert not out[np.broadcast_to(own, out.shape) & some[..., None]].any()
+    # a wrong page among the keys: a whole page's tokens less or more; counts below 2^24 are exact, and so is the maximum, zero
+    n = np.array(lengths)[:, None, None] + np.zeros_like(counts)
+    least = float(c.k_pages.float().min())              # (-30000 as the type holds it)
+    with np.errstate(divide="ignore"):
+        want = np.where(some, np.log(counts), least + np.log(n))
+    got = f64(lse).reshape(counts.shape)
+    assert np.array_equal(np.isneginf(got), n == 0)
+    fine = n > 0
+    within(got[fine], want[fine], (4 * EPS * (1 + np.abs(want)))[fine], "lse")
+
+
+@pytest.mark.parametrize("budget,window", [(600, 0), (30_000, 3), (30_720, 0), (39_000, 8)])
+def test_evict_sequences_that_fit_beside_some_that_do_not(budget, window):
+    """Room for more slots than ranks fit on chip; sequences around that number, and short ones, in one call."""
+    rng = np.random.default_rng([58, budget])
+    lengths, page, dim = [40_000, 30_720, 30_721, 500, 0, 700], 64, 8
+    pages = -(-max(lengths) // page)
+    k = torch.randn((len(lengths) * pages, 1, page, dim), device="cuda")
+    table = dev(rng.permutation(len(lengths) * pages).astype(np.int32).reshape(len(lengths), pages))
+    slots = (len(lengths), 1, pages * page)
+    c = cb.TokenCache(k, torch.randn_like(k), table, dev(np.array(lengths, np.int32)),
+                      dev(rng.integers(0, 3000, slots).astype(np.float32)), dev(rng.integers(0, 1000, slots).astype(np.int32)))
+    check_evict(c, budget, window)
+
+
+def backwards(t, step_tokens=True, step_heads=True):
+    """cb_heads of t's memory read from its last token and head on."""
+    n, heads, dim = t.shape
+    a, b = t.stride()[:2]
+    at = (n - 1) * a * step_tokens + (heads - 1) * b * step_heads
+    return cb.binding.cb_heads(t.data_ptr() + at * t.element_size(), -a if step_tokens else a, -b if step_heads else b, heads, 0)
+
+
+def forwards(t):
+    return cb.binding.cb_heads(t.data_ptr(), t.stride(0), t.stride(1), t.shape[1], 0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tokens,heads", [(True, False), (False, True), (True, True)])
+@pytest.mark.parametrize("pad", [0, 1, 2])
+def test_tensors_in_the_opposite_order(dtype, tokens, heads, pad):
+    """Strides of any sign, in inputs and in outputs (torch has none below zero: through the C ABI)."""
+    rng = np.random.default_rng([59, pad])
+    L, code = cb.lib(), cb.CB_F32 if dtype == F32 else cb.CB_BF16
+    dims, dim, pairs = [d for d, on in ((0, tokens), (1, heads)) if on], 32, (4, 6, 6)
+    stream = torch.cuda.current_stream().cuda_stream
+    wide = lambda n, h: dev(rng.standard_normal((n, h, dim + pad)), dtype)[:, :, :dim]  # noqa: E731
+    n = 37
+    pos, rot = dev(rng.integers(0, 500, (n, 3)).astype(np.int32)), cb.Rotary(dim, pairs)
+    q, k, q_out, k_out = wide(n, 6), wide(n, 2), wide(n, 6), wide(n, 2)
+    assert L.cb_rotate(C.byref(rot.plan), code, n, pos.data_ptr(), C.byref(backwards(q, tokens, heads)), C.byref(forwards(q_out)),
+                       C.byref(forwards(k)), C.byref(backwards(k_out, tokens, heads)), 0, stream) == cb.CB_OK
+    assert torch.equal(q_out, rot.rotate(q.flip(dims), pos))
+    assert torch.equal(k_out, rot.rotate(k, pos).flip(dims))
+
+    a, b = cb.TokenCache.create(1, 2, dim, 64, dtype, 16), cb.TokenCache.create(1, 2, dim, 64, dtype, 16)
+    v, offsets = wide(n, 2), dev(np.array([0, n], np.int32))
+    want = a.append(k.flip(dims), v.flip(dims), pos, rot, q=q, offsets=offsets).flip(dims)
+    assert L.cb_cache_append(C.byref(b.desc), C.byref(rot.plan), n, pos.data_ptr(), offsets.data_ptr(), None, C.byref(backwards(k, tokens, heads)),
+                             C.byref(backwards(v, tokens, heads)), C.byref(forwards(q)), C.byref(backwards(q_out, tokens, heads)), stream) == cb.CB_OK
+    assert torch.equal(q_out, want) and torch.equal(a.k_pages, b.k_pages) and torch.equal(a.v_pages, b.v_pages)
+
+    c = make_cache(rng, [50, 150, 7], 2, dim, 32, dtype)
+    q, out = wide(3, 4), wide(3, 4)
+    c.attend(q)                                         # (its scratch buffer)
+    prm = cb.binding.cb_attend_params(0.25, 0.0, 1.0, 0, 0)
+    want = c.attend(q.flip(dims), scale=0.25)[0].flip(dims)
+    assert L.cb_cache_attend(C.byref(c.desc), C.byref(prm), C.byref(backwards(q, tokens, heads)), C.byref(backwards(out, tokens, heads)), None,
+                             stream) == cb.CB_OK
+    assert torch.equal(out, want)
