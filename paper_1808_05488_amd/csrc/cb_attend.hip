@@ -2,9 +2,9 @@
 //
 // For each sequence and key head: s_j = scale q.k_j for the query heads that read the key head, the softmax over the
 // cached tokens j, and the weighted sum of the v_j.  Keys and values are read once, so memory bounds it: 4 * dim * heads operations for
-// 2 * dim * heads / group values (200 003 tokens of 8 key heads, 128 values in bfloat16: 131 us, 6.2 TB/s, where plain reads reach 7.2; 6.5 over
-// 32 x 8 192 tokens).  One pass: every wavefront takes tiles of consecutive tokens and keeps, for up to 16 query heads, the running maximum m,
-// the sum l of e^(s - m) and the sum o of e^(s - m) v (times a power of two, see Tiles::bits); a tile with a larger maximum scales l and o by e^(m - m').
+// 2 * dim * heads / group values (200 003 tokens of 8 key heads, 128 values in bfloat16: 131 us, 6.3 TB/s, where plain reads reach 7.2; 6.6 over
+// 32 x 8 192 tokens).  More than 16 query heads a key head are blocks of 16, and every block reads the keys and values again.
+// One pass: every wavefront takes tiles of consecutive tokens and keeps, for up to 16 query heads, the running maximum m, the sum l of e^(s - m) and the sum o of e^(s - m) v (times a power of two, see Tiles::bits); a tile with a larger maximum scales l and o by e^(m - m').
 // Parts of a sequence (wavefronts of a workgroup, then workgroups) are joined the same way.
 //
 // Layout.  S^T = K Q^T and O^T = V^T P^T on the matrix cores, 16 query heads as columns.  A lane's column is its query head (lane & 15) in both, so
@@ -18,8 +18,6 @@
 // whole it finishes, and what begins or ends in the middle of something waits in LDS until all wavefronts are through.  What
 // begins or ends in the middle of something for the workgroup goes to the scratch buffer, and the workgroup that comes last of those that
 // share it joins the parts, in order.
-#include <type_traits>
-
 #include "cb_tokens.h"
 
 namespace cb {
@@ -27,14 +25,15 @@ namespace cb {
 namespace {
 
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float LOG2E = 1.44269504088896340736f, LOG2E_REST = (float)(1.44269504088896340736 - (double)LOG2E), LN2 = 0.69314718055994530942f;
 constexpr float LOWEST = -3.402823466e38f;       // of a maximum, so that nothing is subtracted from minus infinity
 constexpr int ROWS = ATTEND_ROWS;
-// Tiles of a wavefront that are worth a workgroup of their own: a part more costs its way through memory and the join.  (Five sequences of 1 - 9 001
-// tokens in float32: 25.8 us with 1, 22.6 with 2, 28.4 with 4; long ones have enough either way.)
+// Tiles of a wavefront that are worth a workgroup of their own: a part more costs its way through memory and the join.  (Measured for five sequences of
+// 1 - 9 001 tokens, float32 and 80 values a head: 25.8 us with 1, 22.6 with 2, 28.4 with 4.  Other head sizes and bfloat16 were not.)
 constexpr int SPLIT_TILES = 2;
 
 struct AttendArgs {
@@ -49,7 +48,8 @@ struct AttendArgs {
 };
 
 // e^x for the difference x of two scores, which is exact or nearly so; scores times log2 e would be rounded at their own size.  What the product is
-// rounded by, and what log2 e is, come in as a factor 1 + rest: without it e^-80 would be off by 2e-6 of itself.
+// rounded by, and what log2 e is, come in as a factor 1 + rest: without it e^-80 would be off by 2e-6 of itself (and five sequences of 1 - 9 001 tokens in
+// float32 take 22.6 us instead of 23.5, 24 in bfloat16 57.9 instead of 58.6).
 __device__ __forceinline__ float exp_of(float x)
 {
     const float y = x * LOG2E, rest = __builtin_fmaf(x, LOG2E_REST, __builtin_fmaf(x, LOG2E, -y)), e = __builtin_amdgcn_exp2f(y);
@@ -59,11 +59,12 @@ __device__ __forceinline__ float exp_of(float x)
 // 2^e, e from -126 to 127.
 __device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
-// Two bfloat16 values, zero in the place of one that is not finite.
+// Two bfloat16 values, the largest finite one of its sign in the place of one that is not finite.  (As integers positive numbers ascend, and so do
+// negative ones that are taken as unsigned.)
 __device__ __forceinline__ uint32_t finite_halves(uint32_t w)
 {
-    const uint32_t odd = ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;       // of a half whose exponent is all ones
-    return w & ~(odd | (odd - (odd >> 15)));
+    const i16x2 x = __builtin_elementwise_min(__builtin_bit_cast(i16x2, w), i16x2{0x7F7F, 0x7F7F});
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, x), u16x2{0xFF7F, 0xFF7F}));
 }
 
 // Part of (sequence, key head, block of query heads) in the scratch buffer: ROWS maxima, ROWS sums, ROWS x DP values.
@@ -414,7 +415,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                 }
             if constexpr (HALF) {
                 // P in three bfloat16 terms of 8 significant bits each, cut off and not rounded: they hold all of a float32's 24 bits, so that P is
-                // no less exact than in float32 (two terms put the sums off by 2^-18 of the values; the third one costs nothing: memory bounds the tile)
+                // no less exact than in float32 (two terms put the sums off by 2^-18 of the values; 200 003 tokens take 133 us instead of 132)
                 uint32_t cut[3][8];
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
@@ -433,44 +434,28 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                     for (int x = 0; x < 4; ++x) w[x] = __builtin_amdgcn_perm(cut[y][2 * x + 1], cut[y][2 * x], 0x07060302u);
                     terms[y] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
                 }
-                // The lower terms may be zero where P is not, and zero times infinity is not a number: where a tile has values that are not
-                // finite (rare, and one question for 64 lanes), the first term alone meets them.
-                u16x2 size = {0, 0};                           // the largest exponents, of both halves of the words
+                // (The lower terms may be zero where P is not, and zero times infinity is not a number: they meet finite values alone.  A branch for tiles that
+                // have others costs registers: 76.7 us instead of 47.1 for 100 000 tokens of 64 values, whose kernel has none left.)
 #pragma unroll
-                for (int s = 0; s < SUB; ++s)
+                for (int pc = 0; pc < NP; ++pc)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
+                    for (int e = 0; e < PE; ++e) {
+                        // value e of the eight tokens, in the order that P has them in
+                        uint32_t w[4];
+                        const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
 #pragma unroll
-                        for (int pc = 0; pc < NP; ++pc)
-#pragma unroll
-                            for (int x = 0; x < DW; ++x) size = __builtin_elementwise_max(size, __builtin_bit_cast(u16x2, v[s][r][pc][x] & 0x7F807F80u));
-                auto add_values = [&](auto all_finite) {
-#pragma unroll
-                    for (int pc = 0; pc < NP; ++pc)
-#pragma unroll
-                        for (int e = 0; e < PE; ++e) {
-                            // value e of the eight tokens, in the order that P has them in
-                            uint32_t w[4];
-                            const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                const int s = x / 2, r = 2 * (x % 2);
-                                w[x] = __builtin_amdgcn_perm(v[s][r + 1][pc][e / 2], v[s][r][pc][e / 2], sel);
-                            }
-                            bf16x8 vt = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-#pragma unroll
-                            for (int y = 0; y < 3; ++y) {
-                                o[pc * PE + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, terms[y], o[pc * PE + e], 0, 0, 0);
-                                if (!all_finite.value && y == 0) {
-#pragma unroll
-                                    for (int x = 0; x < 4; ++x) w[x] = finite_halves(w[x]);
-                                    vt = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-                                }
-                            }
+                        for (int x = 0; x < 4; ++x) {
+                            const int s = x / 2, r = 2 * (x % 2);
+                            w[x] = __builtin_amdgcn_perm(v[s][r + 1][pc][e / 2], v[s][r][pc][e / 2], sel);
                         }
-                };
-                if (__ballot(size[0] == 0x7F80 || size[1] == 0x7F80)) add_values(std::false_type());
-                else add_values(std::true_type());
+                        f32x4& to = o[pc * PE + e];
+                        to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3])), terms[0], to, 0, 0, 0);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) w[x] = finite_halves(w[x]);
+#pragma unroll
+                        for (int y = 1; y < 3; ++y)
+                            to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3])), terms[y], to, 0, 0, 0);
+                    }
             } else {
 #pragma unroll
                 for (int pc = 0; pc < NP; ++pc)
@@ -708,7 +693,7 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
 // weight = decay * weight + the sum over the query heads of a key head of e^(s - m) / l, four slots a thread.  (Not e^(s - lse): the logarithm of l
 // would be rounded at the size of m, and be lost altogether beside a large one.)  A launch of its own, since m and l are
 // only known when all parts are joined: the scores wait in the scratch buffer (4 bytes a query head where keys and values are 4 * dim;
-// 24 sequences of 51 000 tokens in all, 32 query heads: 5 us here, 10 us of the 57 with the scores' way and the launch).
+// 24 sequences of 53 855 tokens in all, 32 query heads: 5 us here, 11 us of the 59 with the scores' way and the launch).
 __global__ __launch_bounds__(256) void weight_kernel(const AttendArgs a)
 {
     const int seq = blockIdx.z, h = blockIdx.y, slot = (blockIdx.x * 256 + threadIdx.x) * 4, len = clamp_length(a.c.lengths[seq], a.c.capacity);
