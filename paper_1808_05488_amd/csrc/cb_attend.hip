@@ -18,6 +18,8 @@
 // whole it finishes, and what begins or ends in the middle of something waits in LDS until all wavefronts are through.  What
 // begins or ends in the middle of something for the workgroup goes to the scratch buffer, and the workgroup that comes last of those that
 // share it joins the parts, in order.
+#include <type_traits>
+
 #include "cb_tokens.h"
 
 namespace cb {
@@ -434,28 +436,46 @@ __global__ __launch_bounds__((Tile<T, DP>::WAVES * 64)) void attend_kernel(const
                     for (int x = 0; x < 4; ++x) w[x] = __builtin_amdgcn_perm(cut[y][2 * x + 1], cut[y][2 * x], 0x07060302u);
                     terms[y] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
                 }
-                // (The lower terms may be zero where P is not, and zero times infinity is not a number: they meet finite values alone.  A branch for tiles that
-                // have others costs registers: 76.7 us instead of 47.1 for 100 000 tokens of 64 values, whose kernel has none left.)
+                // (The lower terms may be zero where P is not, and zero times infinity is not a number: they meet finite values alone.)
+                auto add_values = [&](auto clamp) {
 #pragma unroll
-                for (int pc = 0; pc < NP; ++pc)
+                    for (int pc = 0; pc < NP; ++pc)
 #pragma unroll
-                    for (int e = 0; e < PE; ++e) {
-                        // value e of the eight tokens, in the order that P has them in
-                        uint32_t w[4];
-                        const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+                        for (int e = 0; e < PE; ++e) {
+                            // value e of the eight tokens, in the order that P has them in
+                            uint32_t w[4];
+                            const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const int s = x / 2, r = 2 * (x % 2);
-                            w[x] = __builtin_amdgcn_perm(v[s][r + 1][pc][e / 2], v[s][r][pc][e / 2], sel);
+                            for (int x = 0; x < 4; ++x) {
+                                const int s = x / 2, r = 2 * (x % 2);
+                                w[x] = __builtin_amdgcn_perm(v[s][r + 1][pc][e / 2], v[s][r][pc][e / 2], sel);
+                            }
+                            f32x4& to = o[pc * PE + e];
+                            to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3])), terms[0], to, 0, 0, 0);
+                            if constexpr (clamp.value)
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) w[x] = finite_halves(w[x]);
+#pragma unroll
+                            for (int y = 1; y < 3; ++y)
+                                to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3])), terms[y], to, 0, 0, 0);
                         }
-                        f32x4& to = o[pc * PE + e];
-                        to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3])), terms[0], to, 0, 0, 0);
+                };
+                // Two instructions a word, or a question for 64 lanes and a branch, which takes 60 registers more.  Rows of 65 - 128 values have them: 200 003
+                // tokens 130.6 us with the branch, 135.6 without, 24 streams 48.4 and 49.2.  Up to 64 values some would wait in scratch memory (132.5 and 77.2 us, 54.6
+                // and 36.9), above 128 there is no difference (252.0 and 252.0, 83.1 and 82.8).
+                if constexpr (DP == 128) {
+                    u16x2 size = {0, 0};                       // the largest exponents, of both halves of the words
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) w[x] = finite_halves(w[x]);
+                    for (int s = 0; s < SUB; ++s)
 #pragma unroll
-                        for (int y = 1; y < 3; ++y)
-                            to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3])), terms[y], to, 0, 0, 0);
-                    }
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int pc = 0; pc < NP; ++pc)
+#pragma unroll
+                                for (int x = 0; x < DW; ++x) size = __builtin_elementwise_max(size, __builtin_bit_cast(u16x2, v[s][r][pc][x] & 0x7F807F80u));
+                    if (__ballot(size[0] == 0x7F80 || size[1] == 0x7F80)) add_values(std::true_type());
+                    else add_values(std::false_type());
+                } else add_values(std::true_type());
             } else {
 #pragma unroll
                 for (int pc = 0; pc < NP; ++pc)
