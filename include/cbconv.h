@@ -446,7 +446,8 @@ typedef struct {
                                          by caches whose calls run on one stream.  Calls leave its counters at zero */
     size_t scratch_bytes;
 } cb_cache;
-/* Scratch for all calls on the cache with up to n_q_heads query heads (0: appending and eviction alone). */
+/* Scratch for all calls on the cache with up to n_q_heads query heads (0: appending and eviction alone).  With weight_dev it holds a float for every
+ * query head and slot of the capacity, whether weights are added up or not. */
 int cb_cache_scratch_bytes(const cb_cache *cache, int32_t n_q_heads, size_t *bytes);
 
 /* Append tokens: rows offsets_dev[s] .. offsets_dev[s + 1] - 1 of k and v (n_seq + 1 ascending row numbers from 0 on; NULL: row s
@@ -464,7 +465,8 @@ int cb_cache_append(const cb_cache *cache, const cb_rotary *rotary, int32_t n_to
  *   s_j = scale * q . k_j, capped: softcap * tanh(s_j / softcap) where softcap > 0;  out = sum_j e^(s_j) v_j / sum_j e^(s_j).
  * q->heads is a multiple of n_kv_heads; query head i reads key head i / (q->heads / n_kv_heads).  lse_dev (may be NULL): n_seq x
  * q->heads float32, ln of the sum.  A sequence without a token, or with scores of minus infinity alone, gives zeros and minus
- * infinity.  n_seq * capacity * (key heads times blocks of 16 of their query heads) stays below 2^35.  accumulate = 1 (weight_dev not NULL): weight becomes decay * weight + the sum over the query heads that read it of
+ * infinity.  n_seq * capacity * (key heads times blocks of 16 of their query heads) stays below 2^35; every such block reads the cache once.
+ * accumulate = 1 (weight_dev not NULL): weight becomes decay * weight + the sum over the query heads that read it of
  * e^(s_j - lse), for every slot that holds a token.  The order of the sums depends on
  * lengths, sizes and the GPU's compute units alone.  out overlaps no other array. */
 typedef struct {

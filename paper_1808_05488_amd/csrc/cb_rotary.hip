@@ -3,9 +3,10 @@
 // Pair p of a head, values x and y, turns by position[axis of p] * turns[p] turns: (x cos - y sin, x sin + y cos).  The angle belongs
 // to the token, not to the head, so a workgroup takes a few tokens, computes each of their angles once into LDS, and
 // then streams all heads of those tokens past them.  A value is read once and written once; memory bounds it: 38 400 tokens x 40 heads of 128
-// in bfloat16 129 us (6.1 TB/s, reads and writes; a large copy reaches 5.4), appending 35 000 tokens of 48 heads 172 us (5.0).  The first batch of values
+// in bfloat16 130 us (6.1 TB/s, reads and writes; a large copy reaches 5.4, around the caches 6.4), appending 35 000 tokens of 48 heads 172 us (5.0).  The first batch of values
 // is on its way while the angles are made, and a workgroup ends with one batch: 137 us with four times the tokens.  One token for
-// each of 16 sequences takes 5.6 us, the trips to memory for sequence, page, position and values one after the other.
+// each of 16 sequences takes 5.6 us, the trips to memory for sequence, page, position and values one after the other.  (Appends to slots that are given;
+// behind the tokens that are there, lengths change last: 0.7 us more for the 16 tokens, 2 for 6 126 tokens with a launch of its own.)
 #include "cb_tokens.h"
 
 namespace cb {
