@@ -65,7 +65,10 @@ typedef enum {
     CB_ESTATE = -4    /* call out of order (e.g. pooling before the producer's first frame) */
 } cb_status;
 
-typedef enum { CB_F32 = 0, CB_BF16 = 1 } cb_dtype;
+typedef enum {
+    CB_F32 = 0, CB_BF16 = 1,
+    CB_E4M3 = 8      /* 8 bits, 4 of exponent and 3 of mantissa, no infinities: what a token cache may hold, and nothing else */
+} cb_dtype;
 
 /* Where the layer's change map comes from. */
 typedef enum {
@@ -378,8 +381,8 @@ int cb_select_thresholds(const cb_stage *stages, int32_t n_stages, const void *c
  * say), in a cache of fixed-size pages that one new token per sequence reads and that is cut back to a budget.  These calls
  * keep nothing themselves: every one is described by its arguments, enqueued on hip_stream, asynchronous, and free
  * of allocations, memsets and host decisions that depend on device data, so it may be captured into a HIP graph.
- * Values are float32 or bfloat16; everything between them is computed in float32.  Calls that share a cache or a scratch
- * buffer run on one stream, or are ordered by the caller. */
+ * Values are float32 or bfloat16, a cache may hold them in 8 bits; everything between them is computed in float32 or more.  Calls that
+ * share a cache or a scratch buffer run on one stream, or are ordered by the caller. */
 
 /* A tensor of heads: value i of head h of token n is data_dev[n * token_stride + h * head_stride + i] (strides in values;
  * any sign and order, the values of a head are contiguous).  heads * head_dim values a token. */
@@ -423,13 +426,43 @@ int cb_rotate(const cb_rotary *rotary, int32_t dtype, int64_t n_tokens, const in
               const cb_heads *q, const cb_heads *q_out, const cb_heads *k, const cb_heads *k_out, int32_t inverse,
               void *hip_stream);
 
+/* Norm and rotate: n = x / sqrt(mean(x^2) + eps) for every head x of q (and k), times q_weight_dev (k_weight_dev; head_dim values of weight_dtype, CB_F32
+ * or CB_BF16), then rotated as by cb_rotate and rounded once.  eps >= 0, finite (0: a head of zeros is not a number afterwards).  Mean squares outside
+ * 2^-100 .. 2^100 are computed in float64.  k, k_weight_dev and k_out are NULL together.  An output may be its own input, with its strides. */
+int cb_norm_rotate(const cb_rotary *rotary, int32_t dtype, int64_t n_tokens, const int32_t *positions_dev, float eps,
+                   int32_t weight_dtype, const cb_heads *q, const void *q_weight_dev, const cb_heads *q_out,
+                   const cb_heads *k, const void *k_weight_dev, const cb_heads *k_out, void *hip_stream);
+/* Its gradients, of q, of k or of both (NULL: not this one): x and weight_dev as they went in, out_grad the gradient of what came out; x_grad
+ * (data_dev NULL: not wanted) and weight_grad_dev (NULL: not wanted) receive those of x and of the weight.  Weights' gradients are summed over all tokens and heads in
+ * a fixed order (that depends on sizes and the GPU's compute units alone) and rounded once; with any of them scratch_dev has
+ * cb_norm_rotate_back_scratch_bytes, 16-byte aligned.  x_grad may be out_grad, with its strides, and overlaps no other tensor. */
+typedef struct {
+    cb_heads x, out_grad, x_grad;
+    const void *weight_dev;
+    void *weight_grad_dev;
+} cb_norm_back;
+int cb_norm_rotate_back_scratch_bytes(const cb_rotary *rotary, size_t *bytes);
+int cb_norm_rotate_back(const cb_rotary *rotary, int32_t dtype, int64_t n_tokens, const int32_t *positions_dev, float eps,
+                        int32_t weight_dtype, const cb_norm_back *q, const cb_norm_back *k, void *scratch_dev,
+                        size_t scratch_bytes, void *hip_stream);
+
 /* A paged cache of n_seq sequences.  Slot j of sequence s lies in row j % page_tokens of page table_dev[s * max_pages + j /
  * page_tokens]; a page holds n_kv_heads x page_tokens x head_dim values.  Slots 0 .. lengths_dev[s] - 1 hold tokens, capacity =
  * max_pages * page_tokens is the most.  All arrays belong to the caller, who fills the table (entries behind a sequence's
  * last page are not read) and may change it between calls; a page that is written to belongs to one sequence.  What the
  * host cannot check is checked on the device: lengths are taken as 0 .. capacity, and slots whose page number is
  * not 0 .. n_pages - 1 hold no token: no page is written or read for them, and attention leaves their weight as it is.  (Appending
- * and eviction see to weight and time by slot numbers alone, such slots' too.) */
+ * and eviction see to weight and time by slot numbers alone, such slots' too.)
+ *
+ * A cache of dtype CB_E4M3 holds every value as an e4m3 number times a float32 scale that 16 tokens (slots 16 i .. 16 i + 15) of a page
+ * and key head share, one for keys and one for values.  Keys, values and queries that come and answers that go are of values_dtype, head_dim is a
+ * multiple of 16.  Appending makes the scales: the smallest power of two, 2^-64 .. 2^120, of which 448 times reaches the 16 tokens' largest
+ * finite value, and no smaller than the scale of those among them that are there already, whose values are rounded again where it grows.  Values are
+ * rounded to the nearest, ties to even; infinite ones become 448 times the scale, what is not a number stays so.  Callers may fill pages
+ * and scales (positive, finite) themselves.  Eviction refuses such a cache.
+ *
+ * Bounds (cb_cache_bound, cb_cache_choose) are, for every page and key head, head_dim smallest and head_dim largest values of its tokens'
+ * keys, of the cache's type, with CB_E4M3 bfloat16. */
 typedef struct {
     int32_t n_seq, n_kv_heads;        /* n_seq 1 .. 65535, n_kv_heads 1 .. 1024 */
     int32_t head_dim;                 /* a multiple of 8 up to 256 */
@@ -445,6 +478,10 @@ typedef struct {
     void *scratch_dev;                /* cb_cache_scratch_bytes, 256-byte aligned, cleared to zero by the caller once; shared
                                          by caches whose calls run on one stream.  Calls leave its counters at zero */
     size_t scratch_bytes;
+    int32_t values_dtype;             /* with CB_E4M3: CB_F32 or CB_BF16 */
+    int32_t reserved2;                /* must be zero */
+    float *k_scale_dev, *v_scale_dev; /* with CB_E4M3: n_pages x n_kv_heads x page_tokens / 16 each */
+    void *bounds_dev;                 /* n_pages x n_kv_heads x 2 x head_dim, 16-byte aligned, or NULL */
 } cb_cache;
 /* Scratch for all calls on the cache with up to n_q_heads query heads (0: appending and eviction alone).  With weight_dev it holds a float for every
  * query head and slot of the capacity, whether weights are added up or not. */
@@ -477,6 +514,32 @@ typedef struct {
 } cb_attend_params;
 int cb_cache_attend(const cb_cache *cache, const cb_attend_params *params, const cb_heads *q, const cb_heads *out,
                     float *lse_dev, void *hip_stream);
+
+/* Bring the bounds of pages up to date, of those with slots from since_dev[s] (taken as 0 .. capacity; NULL: 0) to the last token of sequence s: the whole page
+ * that since_dev[s] lies in, too.  Calls that change keys leave bounds as they are: after an append `since` is what it started from; after
+ * an eviction, which moves tokens, it is 0.  A key that is not a number makes its bounds so.  CB_E4M3: rounded outwards to bfloat16 (exact with scales that
+ * appending made).  A page whose bounds are written belongs to one sequence. */
+int cb_cache_bound(const cb_cache *cache, const int32_t *since_dev, void *hip_stream);
+
+/* Choose pages for one new token per sequence (row s of q: sequence s).  The score of a page is the largest, over the query heads that read the key
+ * head, of sum_d max(q_d lo_d, q_d hi_d), which no product of q with a key of the page passes; summed in float64 and rounded to float32, and infinite where
+ * it is not a number.  For every sequence and key head: the `first` first and the `recent` last of its pages, then those with the highest
+ * scores, ties to the lowest, `budget` in all or as many as there are.  chosen_dev (n_seq x n_kv_heads x budget) receives the pages' places in the
+ * sequence's table, ascending, -1 behind them; count_dev (n_seq x n_kv_heads) how many.  Scores grow with the scale of an attention where that is positive. */
+typedef struct {
+    int32_t budget;            /* >= 1 */
+    int32_t first, recent;     /* >= 0, together no more than budget */
+    int32_t reserved;          /* must be zero */
+} cb_choose_params;
+int cb_cache_choose(const cb_cache *cache, const cb_choose_params *params, const cb_heads *q, int32_t *chosen_dev,
+                    int32_t *count_dev, void *hip_stream);
+
+/* cb_cache_attend over the tokens of chosen pages alone: those that row (s, key head) of chosen_dev (rows of `budget`) names, count_dev of
+ * them.  Counts are taken as 0 .. the sequence's pages or budget, whichever is less; places outside 0 .. max_pages - 1 and pages behind the last token hold
+ * no token; a page that is named twice counts twice.  accumulate is refused. */
+int cb_cache_attend_chosen(const cb_cache *cache, const cb_attend_params *params, const cb_heads *q, const cb_heads *out,
+                           float *lse_dev, const int32_t *chosen_dev, const int32_t *count_dev, int32_t budget,
+                           void *hip_stream);
 
 /* Cut every sequence with more than `budget` tokens back to that many, each key head by itself.  Tokens whose time is above the
  * head's newest - window are kept (the newest `budget` where there are more), and of the others those that have had the most

@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcbconv.so")
 
 CB_OK, CB_EINVAL, CB_ENOMEM, CB_EHIP, CB_ESTATE = 0, -1, -2, -3, -4
-CB_F32, CB_BF16 = 0, 1
+CB_F32, CB_BF16, CB_E4M3 = 0, 1, 8
 CB_CLOSED_LOOP, CB_FEED_FORWARD, CB_PROPAGATE = 0, 1, 2
 CB_BACKEND_AUTO, CB_BACKEND_EXPLICIT, CB_BACKEND_FUSED = 0, 1, 2
 CB_NUM_STEPS = 9
@@ -33,7 +33,8 @@ EXPORTS = (
     "cb_pool_destroy", "cb_strerror", "cb_last_hip_error", "cb_version",
     "cb_network_forward", "cb_sum_squared_diff", "cb_sum_squared_diff_noalloc", "cb_select_workspace_bytes",
     "cb_select_thresholds",
-    "cb_rotary_init", "cb_rotate", "cb_cache_scratch_bytes", "cb_cache_append", "cb_cache_attend", "cb_cache_evict",
+    "cb_rotary_init", "cb_rotate", "cb_norm_rotate", "cb_norm_rotate_back_scratch_bytes", "cb_norm_rotate_back",
+    "cb_cache_scratch_bytes", "cb_cache_append", "cb_cache_attend", "cb_cache_bound", "cb_cache_choose", "cb_cache_attend_chosen", "cb_cache_evict",
 )
 CB_METRIC_WORKSPACE_BYTES = 4096
 CB_PAIRS_HALVES, CB_PAIRS_ADJACENT = 0, 1
@@ -73,7 +74,16 @@ class cb_cache(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_seq", "n_kv_heads", "head_dim", "page_tokens", "max_pages", "n_pages",
                                          "dtype", "reserved")] + \
                [(n, C.c_void_p) for n in ("k_pages_dev", "v_pages_dev", "table_dev", "lengths_dev", "weight_dev", "time_dev",
-                                          "scratch_dev")] + [("scratch_bytes", C.c_size_t)]
+                                          "scratch_dev")] + [("scratch_bytes", C.c_size_t), ("values_dtype", C.c_int32), ("reserved2", C.c_int32)] + \
+               [(n, C.c_void_p) for n in ("k_scale_dev", "v_scale_dev", "bounds_dev")]
+
+
+class cb_norm_back(C.Structure):
+    _fields_ = [("x", cb_heads), ("out_grad", cb_heads), ("x_grad", cb_heads), ("weight_dev", C.c_void_p), ("weight_grad_dev", C.c_void_p)]
+
+
+class cb_choose_params(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("budget", "first", "recent", "reserved")]
 
 
 class cb_attend_params(C.Structure):
@@ -156,6 +166,12 @@ def lib():
         L.cb_cache_append.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
         L.cb_cache_attend.argtypes = [vp, vp, vp, vp, vp, vp]
         L.cb_cache_evict.argtypes = [vp, vp, vp]
+        L.cb_norm_rotate.argtypes = [vp, i32, C.c_int64, vp, C.c_float, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.cb_norm_rotate_back_scratch_bytes.argtypes = [vp, P(sz)]
+        L.cb_norm_rotate_back.argtypes = [vp, i32, C.c_int64, vp, C.c_float, i32, vp, vp, vp, sz, vp]
+        L.cb_cache_bound.argtypes = [vp, vp, vp]
+        L.cb_cache_choose.argtypes = [vp, vp, vp, vp, vp, vp]
+        L.cb_cache_attend_chosen.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp]
         L.cb_strerror.argtypes = [C.c_int]
         L.cb_strerror.restype = C.c_char_p
         L.cb_last_hip_error.restype = C.c_int
@@ -628,13 +644,18 @@ class Pool:
 # ---------------------------------------------------------------- tokens of a stream
 # (What keeps addresses of the wrong kind from the GPU is raised, not asserted: it holds under python -O too.)
 _CB_DT = {torch.float32: CB_F32, torch.bfloat16: CB_BF16}
+_E4M3 = torch.float8_e4m3fn
+_BYTE_BLOCK = 16                   # tokens that share a scale of a cache in 8 bits
 # The structures of one call, packed anew for it (a call may run while another thread packs its own).  A call's work on the host is
 # part of a small call's time: packing takes 0.2 us a structure, filling a ctypes one 0.5 us.
 _pack_heads = struct.Struct("@Pqqii").pack
 _pack_attend = struct.Struct("@fffii").pack
 _pack_evict = struct.Struct("@iiPPP").pack
+_pack_two = struct.Struct("@PP").pack
+_pack_choose = struct.Struct("@iiii").pack
 assert struct.calcsize("@Pqqii") == C.sizeof(cb_heads) and struct.calcsize("@fffii") == C.sizeof(cb_attend_params)
-assert struct.calcsize("@iiPPP") == C.sizeof(cb_evict_params)
+assert struct.calcsize("@iiPPP") == C.sizeof(cb_evict_params) and struct.calcsize("@iiii") == C.sizeof(cb_choose_params)
+assert 3 * struct.calcsize("@Pqqii") + 2 * struct.calcsize("@P") == C.sizeof(cb_norm_back)
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -691,6 +712,28 @@ class _Rotation(torch.autograd.Function):
         return None, None, None, back[0], back[1]
 
 
+class _NormRotation(torch.autograd.Function):
+    """Rotary.norm_rotate in a graph."""
+
+    @staticmethod
+    def forward(ctx, rotary, eps, positions, q, q_weight, k, k_weight):
+        ctx.rotary, ctx.eps = rotary, eps
+        ctx.save_for_backward(positions, q, q_weight, k, k_weight)
+        ctx.set_materialize_grads(False)
+        out = rotary.norm_rotate(q, positions, q_weight, k, k_weight, eps)
+        q_out, k_out = (out, None) if k is None else out
+        ctx.mark_non_differentiable(*(y for x, w, y in ((q, q_weight, q_out), (k, k_weight, k_out)) if x is not None and not (x.requires_grad or w.requires_grad)))
+        return q_out, k_out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, q_grad, k_grad):
+        positions, q, q_weight, k, k_weight = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        back = ctx.rotary._norm_back(positions, ctx.eps, (q, q_weight, q_grad, need[3], need[4]), (k, k_weight, k_grad, need[5], need[6]))
+        return (None, None, None) + back
+
+
 class Rotary:
     """Rotary positions with several axes: pairs[a] pairs of a head turn with a token's position on axis a."""
 
@@ -740,22 +783,92 @@ class Rotary:
             _check(status, "cb_rotate")
         return q_out if k is None else (q_out, k_out)
 
+    def norm_rotate(self, q: torch.Tensor, positions: torch.Tensor, q_weight: torch.Tensor, k: Optional[torch.Tensor] = None,
+                    k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+        """Every head of q over the root of its mean square (and eps), times q_weight (head_dim values, float32 or bfloat16), turned by positions as by
+        rotate; k with it by k_weight: q_out, or (q_out, k_out).  q, k and the weights may be parts of a graph (once: gradients of gradients are
+        refused), if their outputs are not given.  An output may be its input."""
+        if (k is None) != (k_weight is None):
+            raise AssertionError("k and k_weight are given together")
+        if torch.is_grad_enabled() and (q.requires_grad or q_weight.requires_grad or (k is not None and (k.requires_grad or k_weight.requires_grad))):
+            if q_out is not None or k_out is not None:
+                raise AssertionError("outputs that are given carry no gradient: norm_rotate without them, or under torch.no_grad()")
+            q_out, k_out = _NormRotation.apply(self, eps, positions, q, q_weight, k, k_weight)
+            return q_out if k is None else (q_out, k_out)
+        if k is None and k_out is not None:
+            raise AssertionError("k_out without k")
+        n, dtype, index, dim, wdtype = q.shape[0], q.dtype, q.get_device(), self.head_dim, q_weight.dtype
+        if index < 0 or dtype not in _CB_DT or wdtype not in _CB_DT:
+            raise AssertionError(f"q: {dtype} on {q.device}, q_weight: {wdtype}; needed: float32 or bfloat16 on a GPU")
+        a, c, d, w = _heads(q, "q", dtype, index, dim), None, None, None
+        if q_out is None:
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            b = _fresh(q_out, dim)
+        else:
+            b = _heads(q_out, "q_out", dtype, index, dim, q.shape[1], n)
+        if k is not None:
+            c, w = _heads(k, "k", dtype, index, dim, None, n), _dense(k_weight, "k_weight", wdtype, index, (dim,))
+            if k_out is None:
+                k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+                d = _fresh(k_out, dim)
+            else:
+                d = _heads(k_out, "k_out", dtype, index, dim, k.shape[1], n)
+        status = lib().cb_norm_rotate(C.byref(self.plan), _CB_DT[dtype], n, _dense(positions, "positions", torch.int32, index, (n, self.n_axes)), eps, _CB_DT[wdtype],
+                                      a, _dense(q_weight, "q_weight", wdtype, index, (dim,)), b, c, w, d, _raw_stream(index))
+        if status:
+            _check(status, "cb_norm_rotate")
+        return q_out if k is None else (q_out, k_out)
+
+    def _norm_back(self, positions, eps, *sides):
+        """Gradients of (x, weight) of each side: (x, weight, gradient of the output or None, whether x's is wanted, the weight's)."""
+        grads, packed, scratch = [], [], None
+        dim, index, wdtype = self.head_dim, positions.get_device(), sides[0][1].dtype
+        n, dtype = sides[0][0].shape[0], sides[0][0].dtype
+        for x, weight, out_grad, of_x, of_weight in sides:
+            if x is None or out_grad is None or not (of_x or of_weight):
+                grads += [None, None]
+                packed.append(None)
+                continue
+            out_grad = out_grad.contiguous()                     # (a gradient comes in any strides)
+            x_grad = torch.empty_like(x, memory_format=torch.contiguous_format) if of_x else None
+            weight_grad = torch.empty_like(weight) if of_weight else None
+            if of_weight and scratch is None:
+                nbytes = C.c_size_t()
+                _check(lib().cb_norm_rotate_back_scratch_bytes(C.byref(self.plan), C.byref(nbytes)), "cb_norm_rotate_back_scratch_bytes")
+                scratch = torch.empty(nbytes.value, dtype=torch.uint8, device=x.device)
+            packed.append(_heads(x, "x", dtype, index, dim) + _heads(out_grad, "gradient", dtype, index, dim, x.shape[1], n) +
+                          (_fresh(x_grad, dim) if of_x else _pack_heads(0, 0, 0, 0, 0)) +
+                          _pack_two(weight.data_ptr(), weight_grad.data_ptr() if of_weight else 0))
+            grads += [x_grad, weight_grad]
+        if any(p is not None for p in packed):
+            status = lib().cb_norm_rotate_back(C.byref(self.plan), _CB_DT[dtype], n, positions.data_ptr(), eps, _CB_DT[wdtype], packed[0], packed[1],
+                                               None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel(), _raw_stream(index))
+            if status:
+                _check(status, "cb_norm_rotate_back")
+        return tuple(grads)
+
 
 class TokenCache:
     """A paged key-value cache (cb_cache) over tensors of the caller's, and its scratch buffer.
 
     k_pages, v_pages: pages x key heads x page_tokens x head_dim; table: sequences x pages of a sequence, int32; lengths:
-    sequences, int32; weight (float32) and time (int32): sequences x key heads x capacity, needed to evict.  scratch, if
+    sequences, int32; weight (float32) and time (int32): sequences x key heads x capacity, needed to evict.  Pages of torch.float8_e4m3fn hold values in 8 bits
+    with k_scale and v_scale (float32: pages x key heads x page_tokens / 16); what comes and goes is float32 or bfloat16 then, call by call.  bounds (pages x key
+    heads x 2 x head_dim, of the pages' type, with 8 bits bfloat16): needed to choose pages.  scratch, if
     it is given (caches may share one): dense uint8, 256-byte aligned, scratch_bytes(query heads) long, and zeroed before the first call.  Calls run on
     the current stream; calls that share a cache or a scratch buffer have to be on one stream, or ordered.  A graph that
     has recorded calls needs the object as long as it is replayed: its scratch buffers stay until then."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
                  weight: Optional[torch.Tensor] = None, time: Optional[torch.Tensor] = None,
-                 scratch: Optional[torch.Tensor] = None):
-        if not (k_pages.is_cuda and k_pages.dim() == 4 and k_pages.dtype in _CB_DT and table.dim() == 2):
-            raise AssertionError(f"k_pages: {k_pages.dtype} {tuple(k_pages.shape)} on {k_pages.device}, table: {tuple(table.shape)}; needed: float32 or "
-                                 f"bfloat16 (pages, key heads, page_tokens, head_dim) on a GPU, and (sequences, pages of a sequence)")
+                 scratch: Optional[torch.Tensor] = None, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
+                 bounds: Optional[torch.Tensor] = None):
+        in_bytes = k_pages.dtype == _E4M3
+        if not (k_pages.is_cuda and k_pages.dim() == 4 and (k_pages.dtype in _CB_DT or in_bytes) and table.dim() == 2):
+            raise AssertionError(f"k_pages: {k_pages.dtype} {tuple(k_pages.shape)} on {k_pages.device}, table: {tuple(table.shape)}; needed: float32, bfloat16 or "
+                                 f"float8_e4m3fn (pages, key heads, page_tokens, head_dim) on a GPU, and (sequences, pages of a sequence)")
+        if (k_scale is not None) != in_bytes or (v_scale is not None) != in_bytes:
+            raise AssertionError(f"k_scale and v_scale belong to pages of float8_e4m3fn, and to no others: these are {k_pages.dtype}")
         n_pages, heads, page, dim = k_pages.shape
         self.n_seq, self.n_kv_heads, self.head_dim, self.capacity = table.shape[0], heads, dim, table.shape[1] * page
         self.device, self.dtype, self._index = k_pages.device, k_pages.dtype, k_pages.get_device()
@@ -763,15 +876,26 @@ class TokenCache:
         i = self._index
         self.desc = d = cb_cache()
         d.n_seq, d.n_kv_heads, d.head_dim, d.page_tokens = self.n_seq, heads, dim, page
-        d.max_pages, d.n_pages, d.dtype = table.shape[1], n_pages, _CB_DT[self.dtype]
+        d.max_pages, d.n_pages, d.dtype = table.shape[1], n_pages, CB_E4M3 if in_bytes else _CB_DT[self.dtype]
         d.k_pages_dev = _dense(k_pages, "k_pages", self.dtype, i, k_pages.shape)
         d.v_pages_dev = _dense(v_pages, "v_pages", self.dtype, i, k_pages.shape)
         d.table_dev = _dense(table, "table", torch.int32, i, table.shape)
         d.lengths_dev = _dense(lengths, "lengths", torch.int32, i, (self.n_seq,))
         d.weight_dev = _dense(weight, "weight", torch.float32, i, self._slots)
         d.time_dev = _dense(time, "time", torch.int32, i, self._slots)
+        blocks = (n_pages, heads, page // _BYTE_BLOCK)
+        d.k_scale_dev, d.v_scale_dev = _dense(k_scale, "k_scale", torch.float32, i, blocks), _dense(v_scale, "v_scale", torch.float32, i, blocks)
+        d.bounds_dev = _dense(bounds, "bounds", torch.bfloat16 if in_bytes else self.dtype, i, (n_pages, heads, 2, dim))
         self.k_pages, self.v_pages, self.table, self.lengths, self.weight, self.time = k_pages, v_pages, table, lengths, weight, time
+        self.k_scale, self.v_scale, self.bounds = k_scale, v_scale, bounds
+        # a structure for each type of what comes and goes (with 8 bits there are two)
+        self._descs = {self.dtype: d}
+        if in_bytes:
+            other = cb_cache.from_buffer_copy(d)
+            d.values_dtype, other.values_dtype = CB_BF16, CB_F32
+            self._descs = {torch.bfloat16: d, torch.float32: other}
         self._address = C.addressof(d)
+        self._addresses = {t: C.addressof(x) for t, x in self._descs.items()}
         self._room = -1                    # query heads that the scratch buffer has room for
         self._outgrown = []                # scratch buffers that graphs and other streams may still use
         self._lse = {}                     # by query heads: what an lse is like
@@ -783,16 +907,24 @@ class TokenCache:
 
     @classmethod
     def create(cls, n_seq: int, n_kv_heads: int, head_dim: int, capacity: int, dtype=torch.bfloat16, page_tokens: int = 64,
-               device="cuda", evictable: bool = True):
-        """An empty cache whose pages belong to the sequences in order."""
+               device="cuda", evictable: Optional[bool] = None, bounded: bool = False):
+        """An empty cache whose pages belong to the sequences in order.  dtype: float32, bfloat16 or float8_e4m3fn.  evictable: with weight and time (not
+        given: where it can be cut back, that is, not in 8 bits); bounded: with bounds, so that pages can be chosen."""
         pages = -(-capacity // page_tokens)
         shape = (n_seq * pages, n_kv_heads, page_tokens, head_dim)
         table = torch.arange(n_seq * pages, dtype=torch.int32, device=device).view(n_seq, pages)
         slots = (n_seq, n_kv_heads, pages * page_tokens)
+        in_bytes = dtype == _E4M3
+        evictable = not in_bytes if evictable is None else evictable
+        if in_bytes and evictable:
+            raise AssertionError("a cache in 8 bits is not cut back: evictable has to be left out, or False")
+        blocks = shape[:2] + (page_tokens // _BYTE_BLOCK,)
+        scales = [torch.ones(blocks, dtype=torch.float32, device=device) if in_bytes else None for _ in range(2)]
         return cls(torch.zeros(shape, dtype=dtype, device=device), torch.zeros(shape, dtype=dtype, device=device), table,
                    torch.zeros(n_seq, dtype=torch.int32, device=device),
                    torch.zeros(slots, dtype=torch.float32, device=device) if evictable else None,
-                   torch.zeros(slots, dtype=torch.int32, device=device) if evictable else None)
+                   torch.zeros(slots, dtype=torch.int32, device=device) if evictable else None, None, *scales,
+                   torch.zeros(shape[:2] + (2, head_dim), dtype=torch.bfloat16 if in_bytes else dtype, device=device) if bounded else None)
 
     def scratch_bytes(self, n_q_heads: int) -> int:
         n = C.c_size_t()
@@ -815,6 +947,15 @@ class TokenCache:
             raise AssertionError(f"scratch: {given.dtype}, strides {given.stride()}, on {given.device}; needed: dense uint8 on {self.device}")
         self.scratch, self._room = given, n_q_heads
         self.desc.scratch_dev, self.desc.scratch_bytes = given.data_ptr(), given.numel()
+        for d in getattr(self, "_descs", {}).values():
+            d.scratch_dev, d.scratch_bytes = self.desc.scratch_dev, self.desc.scratch_bytes
+
+    def _values(self, t: torch.Tensor, what: str):
+        """Type of what a call brings, and the structure for it."""
+        address = self._addresses.get(t.dtype)
+        if address is None:
+            raise AssertionError(f"{what}: {t.dtype}; needed: {' or '.join(str(x) for x in self._addresses)}")
+        return t.dtype, address
 
     def append(self, k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
                q: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None, start: Optional[torch.Tensor] = None,
@@ -824,7 +965,8 @@ class TokenCache:
         sequence's are not written).  Tensors that want a gradient are refused."""
         if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad):
             _refuse_grad("append")
-        n, dtype, i, dim = k.shape[0], self.dtype, self._index, self.head_dim
+        n, i, dim = k.shape[0], self._index, self.head_dim
+        dtype, address = self._values(k, "k")
         a = _heads(k, "k", dtype, i, dim, self.n_kv_heads)
         b = _heads(v, "v", dtype, i, dim, self.n_kv_heads, n)
         c = d = None
@@ -838,7 +980,7 @@ class TokenCache:
         elif q_out is not None:
             raise AssertionError("q_out without q")
         status = lib().cb_cache_append(
-            self._address, None if rotary is None else C.byref(rotary.plan), n if n < 2 ** 31 else -1,
+            address, None if rotary is None else C.byref(rotary.plan), n if n < 2 ** 31 else -1,
             _dense(positions, "positions", torch.int32, i, (n, 1 if rotary is None else rotary.n_axes)),
             _dense(offsets, "offsets", torch.int32, i, (self.n_seq + 1,)), _dense(start, "start", torch.int32, i, (self.n_seq,)),
             a, b, c, d, _raw_stream(i))
@@ -847,14 +989,23 @@ class TokenCache:
         return q_out
 
     def attend(self, q: torch.Tensor, scale: Optional[float] = None, softcap: float = 0.0, accumulate: bool = False,
-               decay: float = 1.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+               decay: float = 1.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, chosen=None):
         """(out, lse) of one query token per sequence (q: sequences x query heads x head_dim).  scale: 1 / sqrt(head_dim) if not
-        given.  accumulate: the cache's weight becomes decay * weight + the weights of this call.  A q that wants a gradient is refused."""
+        given.  accumulate: the cache's weight becomes decay * weight + the weights of this call.  chosen: (chosen, count) as choose gives them, to read
+        those pages alone (and not to accumulate).  A q that wants a gradient is refused."""
         if q.requires_grad:
             _refuse_grad("attend")
-        dtype, i, dim = self.dtype, self._index, self.head_dim
+        i, dim = self._index, self.head_dim
+        dtype, address = self._values(q, "q")
         a = _heads(q, "q", dtype, i, dim, None, self.n_seq)
         heads = q.shape[1]
+        if chosen is not None:
+            pages, count = chosen
+            pairs = (self.n_seq, self.n_kv_heads)
+            if pages.dim() != 3:
+                raise AssertionError(f"chosen: {tuple(pages.shape)}; needed: sequences x key heads x budget")
+            pages_at = _dense(pages, "chosen", torch.int32, i, pairs + (pages.shape[2],))
+            count_at = _dense(count, "count", torch.int32, i, pairs)
         if heads > self._room:
             self._scratch(heads)
         if out is None:
@@ -869,11 +1020,39 @@ class TokenCache:
             lse = torch.empty_like(like)
         else:
             _dense(lse, "lse", torch.float32, i, (self.n_seq, heads))
-        status = lib().cb_cache_attend(self._address, _pack_attend(dim ** -0.5 if scale is None else scale, softcap, decay, 1 if accumulate else 0, 0),
-                                       a, b, lse.data_ptr(), _raw_stream(i))
+        params = _pack_attend(dim ** -0.5 if scale is None else scale, softcap, decay, 1 if accumulate else 0, 0)
+        if chosen is None:
+            status = lib().cb_cache_attend(address, params, a, b, lse.data_ptr(), _raw_stream(i))
+        else:
+            status = lib().cb_cache_attend_chosen(address, params, a, b, lse.data_ptr(), pages_at, count_at, pages.shape[2], _raw_stream(i))
         if status:
-            _check(status, "cb_cache_attend")
+            _check(status, "cb_cache_attend" if chosen is None else "cb_cache_attend_chosen")
         return out, lse
+
+    def bound(self, since: Optional[torch.Tensor] = None) -> None:
+        """Bring the bounds up to date, of the pages with slots from since[s] (int32; not given: 0) to the last token of sequence s: after an append
+        from what it started at, after an eviction all."""
+        i = self._index
+        status = lib().cb_cache_bound(self._address, _dense(since, "since", torch.int32, i, (self.n_seq,)), _raw_stream(i))
+        if status:
+            _check(status, "cb_cache_bound")
+
+    def choose(self, q: torch.Tensor, budget: int, first: int = 0, recent: int = 0):
+        """(chosen, count): for every sequence and key head up to `budget` pages that q can matter to most (q as for attend), by the bounds: the
+        `first` first and the `recent` last ones, then the highest scores; places in the sequence's table, ascending, -1 behind them, and how many."""
+        if q.requires_grad:
+            _refuse_grad("choose")
+        i = self._index
+        dtype, address = self._values(q, "q")
+        a = _heads(q, "q", dtype, i, self.head_dim, None, self.n_seq)
+        if not 1 <= budget < 2 ** 31:
+            raise AssertionError(f"budget: {budget}; needed: 1 or more")
+        chosen = torch.empty((self.n_seq, self.n_kv_heads, budget), dtype=torch.int32, device=self.device)
+        count = torch.empty((self.n_seq, self.n_kv_heads), dtype=torch.int32, device=self.device)
+        status = lib().cb_cache_choose(address, _pack_choose(budget, first, recent, 0), a, chosen.data_ptr(), count.data_ptr(), _raw_stream(i))
+        if status:
+            _check(status, "cb_cache_choose")
+        return chosen, count
 
     def evict(self, budget: int, window: int = 0, weight: Optional[torch.Tensor] = None, time: Optional[torch.Tensor] = None,
               lengths: Optional[torch.Tensor] = None) -> None:

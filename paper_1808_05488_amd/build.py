@@ -13,7 +13,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcbconv.so")
 SOURCES = ["cb_detect.hip", "cb_compact.hip", "cb_gather.hip", "cb_gemm.hip", "cb_fused.hip", "cb_fused_f32.hip", "cb_fused_cl_f32.hip",
-           "cb_fused_cl_bf16.hip", "cb_fused_cl_extract_f32.hip", "cb_fused_cl_extract_bf16.hip", "cb_fused_bf16.hip", "cb_update.hip", "cb_metric.hip", "cb_rotary.hip", "cb_attend.hip",
+           "cb_fused_cl_bf16.hip", "cb_fused_cl_extract_f32.hip", "cb_fused_cl_extract_bf16.hip", "cb_fused_bf16.hip", "cb_update.hip", "cb_metric.hip", "cb_rotary.hip", "cb_norm.hip",
+           "cb_append_bytes.hip", "cb_attend.hip", "cb_attend_bytes.hip", "cb_attend_chosen.hip", "cb_attend_chosen_bytes.hip", "cb_choose.hip",
            "cb_evict.hip", "cb_tokens.hip", "cbconv.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-fast-math", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]
@@ -46,7 +47,8 @@ def spilled_registers(asm: str) -> list[tuple[str, int]]:
 
 
 # sources whose kernels have room for all they hold
-UNSPILLED = {"cb_fused_cl_f32.hip", "cb_fused_cl_extract_f32.hip", "cb_attend.hip"}
+UNSPILLED = {"cb_fused_cl_f32.hip", "cb_fused_cl_extract_f32.hip", "cb_attend.hip", "cb_attend_bytes.hip", "cb_attend_chosen.hip", "cb_attend_chosen_bytes.hip",
+             "cb_norm.hip", "cb_append_bytes.hip", "cb_choose.hip"}
 
 
 def _compile(src: str) -> str:

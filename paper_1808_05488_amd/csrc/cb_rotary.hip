@@ -7,7 +7,7 @@
 // is on its way while the angles are made, and a workgroup ends with one batch: 137 us with four times the tokens.  One token for
 // each of 16 sequences takes 5.6 us, the trips to memory for sequence, page, position and values one after the other.  (Appends to slots that are given;
 // behind the tokens that are there, lengths change last: 0.7 us more for the 16 tokens, 2 for 6 126 tokens with a launch of its own.)
-#include "cb_tokens.h"
+#include "cb_rows.h"
 
 namespace cb {
 
@@ -18,26 +18,8 @@ constexpr int BATCH = 3;                         // items of a thread at a time
 constexpr int MAX_TOKENS = 8;                    // of a workgroup
 constexpr int MAX_ANGLES = 256;                  // of a workgroup
 
-template <typename T, int VE> struct alignas(sizeof(T) * VE) Vec { T e[VE]; };
-
-template <int BYTES> struct Word;
-template <> struct Word<16> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
-template <> struct Word<8> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
-template <> struct Word<4> { typedef uint32_t type; };
-template <> struct Word<2> { typedef uint16_t type; };
 // Values of a rotation pass through once: around the caches (38 400 x 40 heads of 128: 147 -> 137 us).  Those of an append
-// end in rows of many pages, and are better gathered in the caches on their way (35 000 tokens, 48 heads: 176 us, 204 around them).
-template <bool CACHED, typename V> __device__ __forceinline__ V load_once(const void* p)
-{
-    typedef typename Word<sizeof(V)>::type W;
-    return CACHED ? *reinterpret_cast<const V*>(p) : __builtin_bit_cast(V, __builtin_nontemporal_load(reinterpret_cast<const W*>(p)));
-}
-template <bool CACHED, typename V> __device__ __forceinline__ void store_once(const V& v, void* p)
-{
-    typedef typename Word<sizeof(V)>::type W;
-    if (CACHED) *reinterpret_cast<V*>(p) = v;
-    else __builtin_nontemporal_store(__builtin_bit_cast(W, v), reinterpret_cast<W*>(p));
-}
+// end in rows of many pages, and are better gathered in the caches on their way (35 000 tokens, 48 heads: 176 us, 204 around them).  (PAGED says which.)
 
 // Where a token goes in the cache.
 struct Place {
@@ -73,26 +55,10 @@ __device__ void find_place(const RotaryJob& j, const Cache& c, long tok, Place* 
     place->row = ((((long)page * c.heads) << c.page_shift) + (slot & ((1 << c.page_shift) - 1))) * c.dim;
 }
 
-// lengths after the call: start + rows, as far as there are such rows and room
-__device__ void set_lengths(const RotaryJob& j, const Cache& c, int first, int step)
-{
-    for (int s = first; s < c.seqs; s += step) {
-        long rows = 1;
-        if (j.offsets) {
-            const long a = j.offsets[s], b = j.offsets[s + 1] < j.tokens ? j.offsets[s + 1] : j.tokens;
-            rows = b > a ? b - a : 0;
-        }
-        const long n = clamp_length(j.start[s], c.capacity) + rows;
-        c.lengths[s] = n > c.capacity ? c.capacity : (int)n;
-    }
-}
-
 __global__ __launch_bounds__(THREADS) void lengths_kernel(const RotaryJob j, const Cache c)
 {
     set_lengths(j, c, blockIdx.x * THREADS + threadIdx.x, gridDim.x * THREADS);
 }
-
-enum { LENGTHS_LATER = 0, LENGTHS_FIRST = 1 /* first workgroup */, LENGTHS_LAST = 2 /* whoever has read start last */ };
 
 // A workgroup's items are (token, head, piece): two vectors of VE values each.  Of the n pairs of a head, piece p < n / VE turns
 // pairs p * VE .. p * VE + VE - 1; the pieces behind copy what lies behind the pairs, two vectors at a time.  So every
@@ -145,18 +111,10 @@ __global__ __launch_bounds__(THREADS) void rotary_kernel(const RotaryJob j, cons
         find_place(j, c, tok0 + tid - (THREADS - MAX_TOKENS), &place[tid - (THREADS - MAX_TOKENS)]);
     for (int i = tid; i < here * n; i += THREADS) {
         const int t = i / n, p = i - t * n;
-        int axis = 0;
-#pragma unroll
-        for (int a = 0; a < CB_ROTARY_MAX_AXES - 1; ++a) axis += a + 1 < j.axes && p >= j.end[a];
-        // (whole turns go in float64: what is left is exact to float32)
-        double turn = (double)j.positions[(tok0 + t) * j.pos_axes + axis] * j.turns[p];
-        turn -= __builtin_rint(turn);
-        float s, co;
-        sincospif(2.0f * (float)turn, &s, &co);
-        cs[i] = make_float2(co, j.inverse ? -s : s);
+        cs[i] = angle_of(j, tok0 + t, p);
     }
     __syncthreads();
-    if (PAGED && lengths != LENGTHS_LATER) {
+    if (PAGED && (lengths == LENGTHS_FIRST || lengths == LENGTHS_LAST)) {
         if (lengths == LENGTHS_FIRST) {
             if (blockIdx.x == 0) set_lengths(j, c, tid, THREADS);
         } else {
@@ -228,23 +186,6 @@ __global__ __launch_bounds__(THREADS) void rotary_kernel(const RotaryJob j, cons
     }
 }
 
-// Values of a vector: as many as 16 bytes hold, fewer where the pairs, a stride or an address do not divide into such
-// vectors (one value at a time fits everything).
-int vector_values(const RotaryJob& j)
-{
-    const int size = j.bf16 ? 2 : 4;
-    int ve = 16 / size;
-    const Heads* all[] = {&j.q, &j.q_out, &j.k, &j.k_out, &j.v};
-    for (; ve > 1; ve /= 2) {
-        bool fits = j.pairs % ve == 0;
-        for (const Heads* h : all)
-            fits = fits && (h->heads == 0 || !h->data ||
-                            ((uintptr_t)h->data % (size * ve) == 0 && h->token % ve == 0 && h->head % ve == 0));
-        if (fits) break;
-    }
-    return ve;
-}
-
 // Tokens of a workgroup: as many as its threads take in one batch and as it has angles for, as long as there are workgroups for
 // every compute unit left.
 int tokens_of_group(const RotaryJob& j, int pieces)
@@ -260,7 +201,7 @@ int tokens_of_group(const RotaryJob& j, int pieces)
 template <bool PAGED>
 hipError_t launch(const RotaryJob& j, const Cache& c, int lengths, hipStream_t st)
 {
-    const int ve = vector_values(j), pieces = (j.dim + 2 * ve - 1) / (2 * ve), tt = tokens_of_group(j, pieces);
+    const int ve = vector_values<5>(j.bf16, j.pairs, {&j.q, &j.q_out, &j.k, &j.k_out, &j.v}), pieces = (j.dim + 2 * ve - 1) / (2 * ve), tt = tokens_of_group(j, pieces);
     const dim3 grid((unsigned)((j.tokens + tt - 1) / tt)), block(THREADS);
     if (lengths == LENGTHS_LAST && grid.x > 64) lengths = LENGTHS_LATER;
 #define CB_ROTARY(type, n) hipLaunchKernelGGL((rotary_kernel<type, n, PAGED>), grid, block, 0, st, j, c, tt, pieces, lengths)
@@ -307,7 +248,22 @@ hipError_t launch_append(const RotaryJob& j, const Cache& c, hipStream_t st)
         hipLaunchKernelGGL(lengths_kernel, dim3((c.seqs + THREADS - 1) / THREADS), dim3(THREADS), 0, st, j, c);
         return hipGetLastError();
     }
-    return launch<true>(j, c, j.start == c.lengths ? LENGTHS_LAST : LENGTHS_FIRST, st);
+    int lengths = j.start == c.lengths ? LENGTHS_LAST : LENGTHS_FIRST;
+    if (!c.e4m3) return launch<true>(j, c, lengths, st);
+    // 8 bits: queries by themselves, whose rows do not go into the cache
+    hipError_t e = hipSuccess;
+    if (j.q.heads) {
+        RotaryJob q = j;
+        Cache nowhere = c;
+        q.k = q.v = Heads();
+        nowhere.weight = nullptr;
+        nowhere.time = nullptr;
+        e = launch<true>(q, nowhere, LENGTHS_NOT, st);
+    }
+    if (e == hipSuccess) e = launch_append_bytes(j, c, &lengths, st);
+    if (e != hipSuccess || lengths != LENGTHS_LATER) return e;
+    hipLaunchKernelGGL(lengths_kernel, dim3((c.seqs + THREADS - 1) / THREADS), dim3(THREADS), 0, st, j, c);
+    return hipGetLastError();
 }
 
 }  // namespace cb

@@ -17,8 +17,11 @@ struct Heads {
 
 // A cb_cache, checked, with what follows from it.
 struct Cache {
-    int seqs, heads, dim, page_shift, max_pages, n_pages, capacity, bf16;
+    int seqs, heads, dim, page_shift, max_pages, n_pages, capacity, bf16;     // bf16: of the values that come and go (and, without e4m3, are held)
+    int e4m3;                      // held in 8 bits, with scales
     void *k, *v;
+    float *k_scale, *v_scale;
+    void* bounds;
     const int32_t* table;
     int32_t* lengths;
     float* weight;
@@ -37,7 +40,7 @@ constexpr int ATTEND_COUNTERS = 64;
 constexpr int COUNTER_BYTES = (ATTEND_COUNTERS + MAX_GROUPS) * 4;
 
 struct ScratchPlan {
-    size_t parts, sums, scores, moves, total;
+    size_t parts, sums, scores, moves, pages, total;
 };
 ScratchPlan scratch_plan(const Cache& c, int q_heads);
 
@@ -57,15 +60,45 @@ struct RotaryJob {
 constexpr long MOST_TOKENS = (1L << 24) - 1;      // of a launch
 hipError_t launch_rotate(const RotaryJob& j, hipStream_t st);
 hipError_t launch_append(const RotaryJob& j, const Cache& c, hipStream_t st);
+// Who writes the lengths of an append: a launch behind it, its first workgroup, the one that has read start last, nobody.
+enum { LENGTHS_LATER = 0, LENGTHS_FIRST = 1, LENGTHS_LAST = 2, LENGTHS_NOT = 3 };
+// Keys and values into a cache in 8 bits.  lengths: LENGTHS_LATER where it asks for a launch behind it.
+hipError_t launch_append_bytes(const RotaryJob& j, const Cache& c, int* lengths, hipStream_t st);
+
+// Norms of heads with the rotation.  r: its heads (q, k), where they go (q_out, k_out; BACK: the gradients of q and k, turned back: inverse is set).
+constexpr int NORM_GROUPS = 1024;                 // workgroups that leave a row of sums, at most
+struct NormJob {
+    RotaryJob r;
+    const void *q_weight, *k_weight;
+    int weight_bf16;
+    float eps;
+    // backward
+    Heads q_grad, k_grad;          // of q_out and k_out
+    void *q_weight_grad, *k_weight_grad;
+    float* sums;                   // 2 x dim values for every workgroup; null: no gradient of a weight is asked for
+};
+hipError_t launch_norm_rotate(const NormJob& n, hipStream_t st);
+hipError_t launch_norm_rotate_back(const NormJob& n, hipStream_t st);
 
 struct AttendJob {
     Heads q, out;
     float* lse;
     float scale, softcap, decay;
     int accumulate;
+    const int32_t *chosen, *count; // pages of every sequence and key head, `budget` of them at most; null: all
+    int budget;
 };
 bool attend_fits(const Cache& c, int q_heads);      // its work can be counted in 32 bits
 hipError_t launch_attend(const AttendJob& j, const Cache& c, hipStream_t st);
+
+// Bounds of the pages from `since` on (null: of all), and the choice of pages by them.
+struct ChooseJob {
+    Heads q;
+    int budget, first, recent;
+    int32_t *chosen, *count;
+};
+hipError_t launch_bound(const int32_t* since, const Cache& c, hipStream_t st);
+hipError_t launch_choose(const ChooseJob& j, const Cache& c, hipStream_t st);
 
 struct EvictJob {
     int budget, window;
