@@ -5,26 +5,28 @@
 // heads of g n.  Since mean(w g n) = r mean(w g x), both sums over a head are made in one go.
 //
 // Heads are independent and read once, so memory bounds it: 2 values' bytes forward, 3 backward.  A head lies in the registers of 1 - 64 lanes (two
-// vectors of 16 bytes a lane, as pairs need them), its sums take a few steps across them, and a workgroup makes its tokens' angles once for all heads.
+// vectors of 16 bytes a lane, as pairs need them), its sums take a few steps across them.  A wavefront goes through all heads of its tokens by itself: the
+// angles, which it makes once, the weights and all that addresses need stay in its registers.
 // A gradient of the weights is summed in registers by persistent workgroups, each of which leaves one row of sums; a second launch adds these
 // up in order, so that results do not vary.
+#include <climits>
+#include <type_traits>
+
 #include "cb_rows.h"
 
 namespace cb {
 
 namespace {
 
-constexpr int THREADS = 256;
-constexpr int MAX_ANGLES = 512;                  // of a workgroup
-constexpr int MAX_TOKENS = 16;
-constexpr int MAX_DIM = 256;
-// Mean squares in float32 are exact enough, and their root's inverse is a normal number, between these; what is beyond is computed in float64.
+constexpr int THREADS = 256, WAVES = THREADS / 64, MAX_DIM = 256;
+// Mean squares in float32 are exact enough, and their root's inverse is a normal number, between these; what is beyond is scaled by a power of two first.
 constexpr float SMALL = 0x1p-100f, LARGE = 0x1p100f;
 
+// How a wavefront's lanes are dealt: 2^lanes_log to a head, of 2^heads_log heads at a time, of as many tokens as are left over.
 struct Shape {
-    int tokens;                    // of a workgroup at a time
-    int pieces, lanes_log;         // two vectors a piece; lanes of a head
-    long steps;                    // stretches of `tokens`
+    int pieces, lanes_log, heads_log;      // pieces: two vectors each, of a head
+    int q_steps, steps;                    // of 2^heads_log heads: the queries', all
+    long stretches;                        // of a wavefront's tokens
 };
 
 __device__ __forceinline__ float weight_of(const void* w, int bf16, int i)
@@ -32,220 +34,277 @@ __device__ __forceinline__ float weight_of(const void* w, int bf16, int i)
     return bf16 ? widen(((const uint16_t*)w)[i]) : ((const float*)w)[i];
 }
 
-// The sum over the 2^log lanes of a head, the same in each: partners' sums are added in both lanes of a pair.
-__device__ __forceinline__ float head_sum(float v, int log)
+// Over the 2^log lanes of a head, the same in each: partners' values are joined in both lanes of a pair.
+template <typename F> __device__ __forceinline__ float over_head(float v, int log, F join)
 {
-    auto add = [](float a, int b) { return a + __uint_as_float((uint32_t)b); };
-    if (log > 0) v = add(v, __builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0xB1, 0xf, 0xf, true));      // quad_perm 1 0 3 2
-    if (log > 1) v = add(v, __builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x4E, 0xf, 0xf, true));      // quad_perm 2 3 0 1
-    if (log > 2) v = add(v, __builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x141, 0xf, 0xf, true));     // row_half_mirror
-    if (log > 3) v = add(v, __builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x140, 0xf, 0xf, true));     // row_mirror
-    if (log > 4) v += __shfl_xor(v, 16);
-    if (log > 5) v += __shfl_xor(v, 32);
+    auto from = [](int b) { return __uint_as_float((uint32_t)b); };
+    if (log > 0) v = join(v, from(__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0xB1, 0xf, 0xf, true)));      // quad_perm 1 0 3 2
+    if (log > 1) v = join(v, from(__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x4E, 0xf, 0xf, true)));      // quad_perm 2 3 0 1
+    if (log > 2) v = join(v, from(__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x141, 0xf, 0xf, true)));     // row_half_mirror
+    if (log > 3) v = join(v, from(__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x140, 0xf, 0xf, true)));     // row_mirror
+    if (log > 4) v = join(v, __shfl_xor(v, 16));
+    if (log > 5) v = join(v, __shfl_xor(v, 32));
     return v;
 }
-__device__ __forceinline__ double head_sum(double v, int log)
+__device__ __forceinline__ float head_sum(float v, int log) { return over_head(v, log, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ float head_max(float v, int log) { return over_head(v, log, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ int exponent(float v) { return (int)(__float_as_uint(v) >> 23 & 255) - 127; }
+
+// Two vectors of a head's pairs, turned by the lane's angles (see turn() of cb_rows.h for how they lie).
+template <int VE, bool ADJACENT> __device__ __forceinline__ void turn_by(const float2 (&at)[VE], float (&a)[VE], float (&b)[VE])
 {
-    for (int i = 0; i < log; ++i) v += __shfl_xor(v, 1 << i);
-    return v;
+    auto pair = [](float2 cs, float& x, float& y) {
+        const float u = __builtin_fmaf(x, cs.x, -(y * cs.y)), v = __builtin_fmaf(x, cs.y, y * cs.x);
+        x = u;
+        y = v;
+    };
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+        if constexpr (!ADJACENT) pair(at[e], a[e], b[e]);
+        else if (e % 2 == 0) {
+            pair(at[e / 2], a[e], a[(e + 1) % VE]);
+            pair(at[VE / 2 + e / 2], b[e], b[(e + 1) % VE]);
+        }
+    }
 }
 
 // PPL: pieces of a head that a lane has (more than one where single values are taken of heads above 128).
-template <typename T, int VE, int PPL, bool BACK>
+template <typename T, int VE, int PPL, bool ADJACENT, bool BACK>
 __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Shape sh)
 {
     typedef Vec<T, VE> V;
-    // heads of a lane's group that are on their way at once
-    constexpr int BATCH = BACK ? 2 : 3;
-    __shared__ float2 cs[MAX_ANGLES];
+    typedef typename Word<sizeof(V)>::type W;
+    constexpr int BATCH = BACK ? 2 : 3;          // steps that are on their way at once
+    extern __shared__ __align__(16) float2 s_dyn[];      // a wavefront's angles; BACK: its sums in the end
     __shared__ __align__(16) float s_w[2][MAX_DIM];
-    extern __shared__ float s_sum[];             // BACK: 2 * VE * PPL values of every thread
     const RotaryJob& j = n.r;
-    const int tid = threadIdx.x, np = j.pairs, dim = j.dim, hq = j.q.heads, heads = hq + j.k.heads;
-    const int lanes_log = sh.lanes_log, group = tid >> lanes_log, groups = THREADS >> lanes_log, sub = tid & ((1 << lanes_log) - 1);
-    const int turned = np / VE;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), np = j.pairs, dim = j.dim;
+    const int log = sh.lanes_log, sub = lane & ((1 << log) - 1), slot = lane >> log, head0 = slot & ((1 << sh.heads_log) - 1), token = slot >> sh.heads_log;
+    const int tokens = (64 >> log) >> sh.heads_log, turned = np / VE;
     const float scale = 1.0f / (float)dim;
+    float2* s_cs = s_dyn + wave * tokens * np;
     for (int i = tid; i < 2 * dim; i += THREADS) {
-        const void* w = i < dim ? n.q_weight : n.k_weight;
+        const void* from = i < dim ? n.q_weight : n.k_weight;
         const int d = i < dim ? i : i - dim;
-        s_w[i < dim ? 0 : 1][d] = w ? weight_of(w, n.weight_bf16, d) : 0.0f;
+        s_w[i < dim ? 0 : 1][d] = from ? weight_of(from, n.weight_bf16, d) : 0.0f;
     }
+    __syncthreads();
     // where a lane's pieces lie in a head, the same of every head
     int first[PPL], second[PPL];
     bool turns[PPL], has_a[PPL], has_b[PPL];
 #pragma unroll
     for (int p = 0; p < PPL; ++p) {
-        const int piece = sub + (p << lanes_log);
+        const int piece = sub + (p << log);
         turns[p] = piece < turned;
         first[p] = turns[p] && !j.adjacent ? VE * piece : 2 * VE * piece;
         second[p] = turns[p] && !j.adjacent ? np + VE * piece : 2 * VE * piece + VE;
         has_a[p] = piece < sh.pieces;
         has_b[p] = has_a[p] && second[p] < dim;
     }
-    float sum_q[PPL][2][VE] = {}, sum_k[PPL][2][VE] = {};        // BACK: of g n, of all heads that were here
+    float sum[2][PPL][2][VE] = {};               // BACK: of g n, of all heads that were here
 
-    for (long step = blockIdx.x; step < sh.steps; step += gridDim.x) {
-        const long tok0 = step * sh.tokens;
-        const int here = (int)(j.tokens - tok0 < sh.tokens ? j.tokens - tok0 : sh.tokens), rows = here * heads;
-        V x[BATCH][PPL][2], g[BATCH][PPL][2];
+    for (long stretch = (long)blockIdx.x * WAVES + wave; stretch < sh.stretches; stretch += (long)gridDim.x * WAVES) {
+        const long tok = stretch * tokens + token;
+        const bool real = tok < j.tokens;
+        W x[BATCH][PPL][2], g[BATCH][PPL][2];
+        // (by value: a choice between the arguments' addresses would put them all into scratch memory)
+        auto head_at = [&](bool q, Heads a, Heads b, int h) {
+            return (const T*)(q ? a.data : b.data) + tok * (q ? a.token : b.token) + (long)h * (q ? a.head : b.head);
+        };
+        auto get = [](bool there, const T* from) {
+            W v = W{};
+            if (there) v = __builtin_nontemporal_load(reinterpret_cast<const W*>(from));
+            return v;
+        };
         auto fetch = [&](int base) {
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) {
-                const int row = base + u * groups, t = row / heads, h = row - t * heads;
-                const bool q = h < hq, there = row < rows;
-                const Heads& from = q ? j.q : j.k;
-                const T* src = (const T*)from.data + (tok0 + t) * from.token + (long)(q ? h : h - hq) * from.head;
-                const Heads& grad = q ? n.q_grad : n.k_grad;
-                const T* gsrc = BACK ? (const T*)grad.data + (tok0 + t) * grad.token + (long)(q ? h : h - hq) * grad.head : nullptr;
+                const int step = base + u;
+                if (step >= sh.steps) continue;
+                const bool q = step < sh.q_steps;
+                const int h = head0 + ((q ? step : step - sh.q_steps) << sh.heads_log);
+                const bool there = real && h < (q ? j.q.heads : j.k.heads);
+                const T *src = head_at(q, j.q, j.k, h), *gsrc = BACK ? head_at(q, n.q_grad, n.k_grad, h) : nullptr;
 #pragma unroll
                 for (int p = 0; p < PPL; ++p) {
-                    x[u][p][0] = x[u][p][1] = V{};
-                    if (there && has_a[p]) x[u][p][0] = load_once<false, V>(src + first[p]);
-                    if (there && has_b[p]) x[u][p][1] = load_once<false, V>(src + second[p]);
+                    x[u][p][0] = get(there && has_a[p], src + first[p]);
+                    x[u][p][1] = get(there && has_b[p], src + second[p]);
                     if constexpr (BACK) {
-                        g[u][p][0] = g[u][p][1] = V{};
-                        if (there && has_a[p]) g[u][p][0] = load_once<false, V>(gsrc + first[p]);
-                        if (there && has_b[p]) g[u][p][1] = load_once<false, V>(gsrc + second[p]);
+                        g[u][p][0] = get(there && has_a[p], gsrc + first[p]);
+                        g[u][p][1] = get(there && has_b[p], gsrc + second[p]);
                     }
                 }
             }
         };
-        fetch(group);
-        __syncthreads();                         // the last stretch's angles have been used
-        for (int i = tid; i < here * np; i += THREADS) {
-            const int t = i / np;
-            cs[i] = angle_of(j, tok0 + t, i - t * np);
+        fetch(0);
+        float2 at[PPL][VE];
+        {
+            // (the last stretch's angles have been read: a wavefront's accesses of LDS are in order)
+            for (int i = lane; i < tokens * np; i += 64) {
+                const int t = i / np;
+                const long y = stretch * tokens + t;
+                s_cs[i] = angle_of(j, y < j.tokens ? y : j.tokens - 1, i - t * np);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+            for (int p = 0; p < PPL; ++p)
+#pragma unroll
+                for (int e = 0; e < VE; ++e) at[p][e] = turns[p] ? s_cs[token * np + (sub + (p << log)) * VE + e] : make_float2(1.0f, 0.0f);
+            __builtin_amdgcn_wave_barrier();
         }
-        __syncthreads();
-        for (int base = group; base - group < rows;) {
+        auto take = [&](int u, int step, auto side_is) {
+            constexpr int side = side_is.value;
+            const int h = head0 + ((side ? step - sh.q_steps : step) << sh.heads_log);
+            const bool there = real && h < (side ? j.k.heads : j.q.heads);
+            float f[PPL][2][VE], d[PPL][2][VE], w[PPL][2][VE];       // the head; BACK: its gradient, turned back; the weights
+            float squares = 0.0f, dot = 0.0f;
 #pragma unroll
-            for (int u = 0; u < BATCH; ++u) {
-                const int row = base + u * groups, t = row / heads, h = row - t * heads;
-                const bool q = h < hq, there = row < rows;
-                if (base - group + u * groups >= rows) break;        // (the same for all: lanes of a head add up together)
-                const float* w = s_w[q ? 0 : 1];
-                const float2* at = cs + (there ? t : 0) * np;
-                float f[PPL][2][VE], d[PPL][2][VE];                  // the head; BACK: w times its gradient, turned back
-                float squares = 0.0f, dot = 0.0f;
+            for (int p = 0; p < PPL; ++p) {
+                const V xa = __builtin_bit_cast(V, x[u][p][0]), xb = __builtin_bit_cast(V, x[u][p][1]);
+                V ga = {}, gb = {};
+                if constexpr (BACK) { ga = __builtin_bit_cast(V, g[u][p][0]); gb = __builtin_bit_cast(V, g[u][p][1]); }
 #pragma unroll
-                for (int p = 0; p < PPL; ++p) {
+                for (int e = 0; e < VE; ++e) {
+                    w[p][0][e] = has_a[p] ? s_w[side][first[p] + e] : 0.0f;
+                    w[p][1][e] = has_b[p] ? s_w[side][second[p] + e] : 0.0f;
+                    f[p][0][e] = widen(xa.e[e]);
+                    f[p][1][e] = widen(xb.e[e]);
+                    if constexpr (BACK) {
+                        d[p][0][e] = widen(ga.e[e]);
+                        d[p][1][e] = widen(gb.e[e]);
+                    }
+                    squares = __builtin_fmaf(f[p][0][e], f[p][0][e], squares);
+                    squares = __builtin_fmaf(f[p][1][e], f[p][1][e], squares);
+                }
+                if constexpr (BACK) {
+                    turn_by<VE, ADJACENT>(at[p], d[p][0], d[p][1]);
 #pragma unroll
                     for (int e = 0; e < VE; ++e) {
-                        f[p][0][e] = widen(x[u][p][0].e[e]);
-                        f[p][1][e] = widen(x[u][p][1].e[e]);
-                        if constexpr (BACK) {
-                            d[p][0][e] = widen(g[u][p][0].e[e]);
-                            d[p][1][e] = widen(g[u][p][1].e[e]);
-                        }
-                        squares += f[p][0][e] * f[p][0][e];
-                        squares += f[p][1][e] * f[p][1][e];
+                        dot = __builtin_fmaf(w[p][0][e] * d[p][0][e], f[p][0][e], dot);
+                        dot = __builtin_fmaf(w[p][1][e] * d[p][1][e], f[p][1][e], dot);
                     }
-                    if constexpr (BACK) {
-                        if (turns[p]) turn<VE>(at + (sub + (p << lanes_log)) * VE, j.adjacent, d[p][0], d[p][1]);
-#pragma unroll
-                        for (int e = 0; e < VE; ++e) {
-                            if (has_a[p]) dot += w[first[p] + e] * d[p][0][e] * f[p][0][e];
-                            if (has_b[p]) dot += w[second[p] + e] * d[p][1][e] * f[p][1][e];
-                        }
-                    }
-                }
-                squares = head_sum(squares, lanes_log);
-                const float mean = squares * scale + n.eps;
-                float r = 0.0f;
-                double r64 = 0.0, dot64 = 0.0;
-                const bool far = !(mean >= SMALL && mean <= LARGE);
-                if (!far) {
-                    r = 1.0f / sqrtf(mean);
-                    if constexpr (BACK) dot = head_sum(dot, lanes_log) * r * scale;
-                } else {
-                    double sum = 0.0;
-#pragma unroll
-                    for (int p = 0; p < PPL; ++p)
-#pragma unroll
-                        for (int e = 0; e < VE; ++e) {
-                            sum += (double)f[p][0][e] * f[p][0][e] + (double)f[p][1][e] * f[p][1][e];
-                            if constexpr (BACK) {
-                                if (has_a[p]) dot64 += (double)w[first[p] + e] * d[p][0][e] * f[p][0][e];
-                                if (has_b[p]) dot64 += (double)w[second[p] + e] * d[p][1][e] * f[p][1][e];
-                            }
-                        }
-                    r64 = 1.0 / sqrt(head_sum(sum, lanes_log) / dim + (double)n.eps);
-                    dot64 = head_sum(dot64, lanes_log) * r64 / dim;
-                }
-                const Heads& to = q ? j.q_out : j.k_out;
-                T* dst = (T*)to.data + (tok0 + t) * to.token + (long)(q ? h : h - hq) * to.head;
-#pragma unroll
-                for (int p = 0; p < PPL; ++p) {
-#pragma unroll
-                    for (int e = 0; e < VE; ++e)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int at = (i ? second[p] : first[p]) + e;
-                            const float wi = (i ? has_b[p] : has_a[p]) ? w[at] : 0.0f;
-                            if constexpr (!BACK) f[p][i][e] = far ? (float)((double)f[p][i][e] * r64 * wi) : f[p][i][e] * r * wi;
-                            else {
-                                const float norm = far ? (float)((double)f[p][i][e] * r64) : f[p][i][e] * r, part = d[p][i][e] * norm;
-                                if (q) sum_q[p][i][e] += there ? part : 0.0f;
-                                else sum_k[p][i][e] += there ? part : 0.0f;
-                                f[p][i][e] = far ? (float)(r64 * ((double)wi * d[p][i][e] - norm * dot64)) : r * (wi * d[p][i][e] - norm * dot);
-                            }
-                        }
-                    if (!BACK && turns[p]) turn<VE>(at + (sub + (p << lanes_log)) * VE, j.adjacent, f[p][0], f[p][1]);
-                    if (!there || !to.data) continue;
-                    V y, z;
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) { narrow(f[p][0][e], y.e[e]); narrow(f[p][1][e], z.e[e]); }
-                    if (has_a[p]) store_once<false>(y, dst + first[p]);
-                    if (has_b[p]) store_once<false>(z, dst + second[p]);
                 }
             }
-            base += BATCH * groups;
-            if (base - group < rows) fetch(base);
+            squares = head_sum(squares, log);
+            if constexpr (BACK) dot = head_sum(dot, log);
+            float mean = __builtin_fmaf(squares, scale, n.eps);
+            int down = 0;                                            // f is the head times 2^-down
+            if (!(mean >= SMALL && mean <= LARGE)) {
+                float top = 0.0f;
+#pragma unroll
+                for (int p = 0; p < PPL; ++p)
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) top = fmaxf(top, fmaxf(fabsf(f[p][0][e]), fabsf(f[p][1][e])));
+                const int e0 = exponent(head_max(top, log)), e1 = n.eps > 0.0f ? exponent(n.eps) / 2 : -127;
+                down = e0 > e1 ? e0 : e1;
+                squares = dot = 0.0f;
+#pragma unroll
+                for (int p = 0; p < PPL; ++p)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) {
+                            f[p][i][e] = __builtin_ldexpf(f[p][i][e], -down);
+                            squares = __builtin_fmaf(f[p][i][e], f[p][i][e], squares);
+                            if constexpr (BACK) dot = __builtin_fmaf(w[p][i][e] * d[p][i][e], f[p][i][e], dot);
+                        }
+                squares = head_sum(squares, log);
+                if constexpr (BACK) dot = head_sum(dot, log);
+                mean = __builtin_fmaf(squares, scale, __builtin_ldexpf(n.eps, -2 * down));
+            }
+            const float r = __builtin_amdgcn_rsqf(mean);             // (within one unit in the last place)
+            if constexpr (BACK) dot = dot * r * scale;
+            T* dst = (T*)head_at(!side, j.q_out, j.k_out, h);
+            const bool stored = (side ? j.k_out.data : j.q_out.data) != nullptr;
+#pragma unroll
+            for (int p = 0; p < PPL; ++p) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) {
+                        const float norm = f[p][i][e] * r;
+                        if constexpr (!BACK) f[p][i][e] = norm * w[p][i][e];
+                        else {
+                            const float part = d[p][i][e] * norm;
+                            sum[side][p][i][e] += there ? part : 0.0f;
+                            f[p][i][e] = r * __builtin_fmaf(-norm, dot, w[p][i][e] * d[p][i][e]);
+                            if (down != 0) f[p][i][e] = __builtin_ldexpf(f[p][i][e], -down);
+                        }
+                    }
+                if constexpr (!BACK) turn_by<VE, ADJACENT>(at[p], f[p][0], f[p][1]);
+                if (!there || !stored) continue;
+                V y, z;
+#pragma unroll
+                for (int e = 0; e < VE; ++e) { narrow(f[p][0][e], y.e[e]); narrow(f[p][1][e], z.e[e]); }
+                if (has_a[p]) store_once<false>(y, dst + first[p]);
+                if (has_b[p]) store_once<false>(z, dst + second[p]);
+            }
+        };
+        for (int base = 0; base < sh.steps;) {
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                if (base + u >= sh.steps) continue;
+                if (base + u < sh.q_steps) take(u, base + u, std::integral_constant<int, 0>());
+                else take(u, base + u, std::integral_constant<int, 1>());
+            }
+            base += BATCH;
+            if (base < sh.steps) fetch(base);
         }
     }
     if constexpr (BACK) {
         if (!n.sums) return;
-        // this workgroup's row of sums: over its groups of lanes, in order
-        constexpr int OWN = 2 * VE * PPL;
+        // this workgroup's row of sums: over the slots of a wavefront, pair by pair, then over its wavefronts
+        __syncthreads();
+        float* s_sum = reinterpret_cast<float*>(s_dyn);
 #pragma unroll
-        for (int side = 0; side < 2; ++side) {
-            __syncthreads();
+        for (int side = 0; side < 2; ++side)
 #pragma unroll
             for (int p = 0; p < PPL; ++p)
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int e = 0; e < VE; ++e) s_sum[((p * 2 + i) * VE + e) * THREADS + tid] = side ? sum_k[p][i][e] : sum_q[p][i][e];
-            __syncthreads();
-            for (int o = tid; o < OWN << lanes_log; o += THREADS) {
-                const int slot = o >> lanes_log, lane = o & ((1 << lanes_log) - 1), e = slot % VE, i = slot / VE % 2, piece = lane + ((slot / (2 * VE)) << lanes_log);
-                if (piece >= sh.pieces) continue;
-                const bool t = piece < turned && !j.adjacent;
-                const int d = (i == 0 ? (t ? VE * piece : 2 * VE * piece) : (t ? np + VE * piece : 2 * VE * piece + VE)) + e;
-                if (d >= dim) continue;
-                float sum = 0.0f;
-                for (int y = 0; y < groups; ++y) sum += s_sum[slot * THREADS + (y << lanes_log) + lane];
-                n.sums[((long)blockIdx.x * 2 + side) * dim + d] = sum;
-            }
+                    for (int e = 0; e < VE; ++e) {
+                        float v = sum[side][p][i][e];
+                        for (int k = log; k < 6; ++k) v += __shfl_xor(v, 1 << k);
+                        const int d = (i ? second[p] : first[p]) + e;
+                        const bool has = i ? has_b[p] : has_a[p];
+                        if (slot == 0 && has) s_sum[(wave * 2 + side) * dim + d] = v;
+                    }
+        __syncthreads();
+        for (int d = tid; d < 2 * dim; d += THREADS) {
+            float v = 0.0f;
+            for (int k = 0; k < WAVES; ++k) v += s_sum[k * 2 * dim + d];
+            n.sums[(long)blockIdx.x * 2 * dim + d] = v;
         }
     }
 }
 
-// The workgroups' rows of sums, added up: 16 columns a workgroup, 16 threads a column, each of which takes every 16th row.
-__global__ __launch_bounds__(256) void sums_kernel(const NormJob n, int rows)
+// The workgroups' rows of sums, added up: 16 columns a workgroup, 64 threads a column, each of which takes every 64th row.
+constexpr int COLUMNS = 16, TEAMS = 64;
+__global__ __launch_bounds__(COLUMNS * TEAMS) void sums_kernel(const NormJob n, int rows)
 {
-    __shared__ double s_part[16][16];
-    const int dim = n.r.dim, col = blockIdx.x * 16 + (threadIdx.x & 15), team = threadIdx.x >> 4;
+    __shared__ double s_part[TEAMS][COLUMNS + 1];
+    const int dim = n.r.dim, x = threadIdx.x % COLUMNS, col = blockIdx.x * COLUMNS + x, team = threadIdx.x / COLUMNS;
+    float v[NORM_GROUPS / TEAMS];
+#pragma unroll
+    for (int i = 0; i < NORM_GROUPS / TEAMS; ++i) {
+        const int row = team + TEAMS * i;
+        v[i] = col < 2 * dim && row < rows ? n.sums[(long)row * 2 * dim + col] : 0.0f;
+    }
     double sum = 0.0;
-    if (col < 2 * dim)
-        for (int i = team; i < rows; i += 16) sum += n.sums[(long)i * 2 * dim + col];
-    s_part[team][threadIdx.x & 15] = sum;
-    __syncthreads();
-    if (team != 0 || col >= 2 * dim) return;
-    for (int i = 1; i < 16; ++i) sum += s_part[i][threadIdx.x & 15];
+#pragma unroll
+    for (int i = 0; i < NORM_GROUPS / TEAMS; ++i) sum += v[i];
+    s_part[team][x] = sum;
+    for (int half = TEAMS / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (team < half) s_part[team][x] += s_part[team + half][x];
+    }
     void* to = col < dim ? n.q_weight_grad : n.k_weight_grad;
+    if (team != 0 || col >= 2 * dim || !to) return;
     const int d = col < dim ? col : col - dim;
-    if (!to) return;
+    sum = s_part[0][x];
     if (n.weight_bf16) narrow((float)sum, ((uint16_t*)to)[d]);
     else ((float*)to)[d] = (float)sum;
 }
@@ -253,35 +312,47 @@ __global__ __launch_bounds__(256) void sums_kernel(const NormJob n, int rows)
 template <bool BACK> hipError_t launch(const NormJob& n, hipStream_t st)
 {
     const RotaryJob& j = n.r;
-    const int ve = vector_values<6>(j.bf16, j.pairs, {&j.q, &j.q_out, &j.k, &j.k_out, &n.q_grad, &n.k_grad});
+    const int ve = vector_values<6>(j.bf16, j.pairs, {&j.q, &j.q_out, &j.k, &j.k_out, &n.q_grad, &n.k_grad}), units = device_units();
     Shape sh;
     sh.pieces = (j.dim + 2 * ve - 1) / (2 * ve);
     sh.lanes_log = 0;
     while (1 << sh.lanes_log < sh.pieces && sh.lanes_log < 6) ++sh.lanes_log;
-    const int heads = j.q.heads + j.k.heads, at_once = (BACK ? 2 : 3) * (THREADS >> sh.lanes_log), angles = MAX_ANGLES / j.pairs, units = device_units();
-    int tt = at_once / heads;
-    tt = tt < angles ? tt : angles;
-    tt = tt < 1 ? 1 : (tt > MAX_TOKENS ? MAX_TOKENS : tt);
-    while (tt > 1 && j.tokens / tt < 4L * units) tt /= 2;
-    sh.tokens = tt;
-    sh.steps = (j.tokens + tt - 1) / tt;
-    const long most = BACK ? NORM_GROUPS : 1L << 22;
-    const dim3 grid((unsigned)(sh.steps < most ? sh.steps : most)), block(THREADS);
-#define CB_NORM(type, v, p) hipLaunchKernelGGL((norm_kernel<type, v, p, BACK>), grid, block, BACK ? 2 * v * p * THREADS * sizeof(float) : 0, st, n, sh)
-    if (j.bf16) {
-        if (ve == 8) CB_NORM(uint16_t, 8, 1);
-        else if (ve == 4) CB_NORM(uint16_t, 4, 1);
-        else if (ve == 2) CB_NORM(uint16_t, 2, 1);
-        else CB_NORM(uint16_t, 1, 2);
-    } else {
-        if (ve == 4) CB_NORM(float, 4, 1);
-        else if (ve == 2) CB_NORM(float, 2, 1);
-        else CB_NORM(float, 1, 2);
+    // heads at a time: as many as leave the fewest lanes without one
+    long least = LONG_MAX;
+    for (int log = 0; log <= 6 - sh.lanes_log; ++log) {
+        const int q = (j.q.heads + (1 << log) - 1) >> log, k = (j.k.heads + (1 << log) - 1) >> log;
+        const long cost = (long)(q + k) << log;
+        if (cost > least) continue;
+        least = cost;
+        sh.heads_log = log;
+        sh.q_steps = q;
+        sh.steps = q + k;
     }
+    const int tokens = (64 >> sh.lanes_log) >> sh.heads_log;
+    sh.stretches = (j.tokens + tokens - 1) / tokens;
+    // backward as many workgroups as are at work at once: eight values a vector take registers for two a compute unit, fewer for three and more (19 200 tokens,
+    // 40 heads of 128 in bfloat16: 125 us with 2, 160 with 3, 134 with 4); forward a wavefront for every stretch (129 us, 136 - 143 with fewer)
+    const long groups = (sh.stretches + WAVES - 1) / WAVES, at_once = (ve == 8 ? 2L : 3L) * units, most = BACK ? (at_once < NORM_GROUPS ? at_once : NORM_GROUPS) : 1L << 22;
+    const dim3 grid((unsigned)(groups < most ? groups : most)), block(THREADS);
+    size_t lds = (size_t)WAVES * tokens * j.pairs * sizeof(float2);
+    if (BACK && lds < WAVES * 2 * j.dim * sizeof(float)) lds = WAVES * 2 * j.dim * sizeof(float);
+#define CB_NORM(type, v, p, adjacent) hipLaunchKernelGGL((norm_kernel<type, v, p, adjacent, BACK>), grid, block, lds, st, n, sh)
+#define CB_NORMS(type, v) do { if (j.adjacent) CB_NORM(type, v, 1, true); else CB_NORM(type, v, 1, false); } while (0)
+    if (j.bf16) {
+        if (ve == 8) CB_NORMS(uint16_t, 8);
+        else if (ve == 4) CB_NORMS(uint16_t, 4);
+        else if (ve == 2) CB_NORMS(uint16_t, 2);
+        else CB_NORM(uint16_t, 1, 2, false);
+    } else {
+        if (ve == 4) CB_NORMS(float, 4);
+        else if (ve == 2) CB_NORMS(float, 2);
+        else CB_NORM(float, 1, 2, false);
+    }
+#undef CB_NORMS
 #undef CB_NORM
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !BACK || !n.sums) return e;
-    hipLaunchKernelGGL(sums_kernel, dim3((2 * j.dim + 15) / 16), dim3(256), 0, st, n, (int)grid.x);
+    hipLaunchKernelGGL(sums_kernel, dim3((2 * j.dim + COLUMNS - 1) / COLUMNS), dim3(COLUMNS * TEAMS), 0, st, n, (int)grid.x);
     return hipGetLastError();
 }
 
@@ -294,7 +365,7 @@ hipError_t launch_norm_rotate_back(const NormJob& n, hipStream_t st)
 {
     if (n.r.tokens) return launch<true>(n, st);
     if (!n.sums) return hipSuccess;
-    hipLaunchKernelGGL(sums_kernel, dim3((2 * n.r.dim + 15) / 16), dim3(256), 0, st, n, 0);
+    hipLaunchKernelGGL(sums_kernel, dim3((2 * n.r.dim + COLUMNS - 1) / COLUMNS), dim3(COLUMNS * TEAMS), 0, st, n, 0);
     return hipGetLastError();
 }
 
