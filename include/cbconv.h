@@ -434,7 +434,7 @@ int cb_norm_rotate(const cb_rotary *rotary, int32_t dtype, int64_t n_tokens, con
                    const cb_heads *k, const void *k_weight_dev, const cb_heads *k_out, void *hip_stream);
 /* Its gradients, of q, of k or of both (NULL: not this one): x and weight_dev as they went in, out_grad the gradient of what came out; x_grad
  * (data_dev NULL: not wanted) and weight_grad_dev (NULL: not wanted) receive those of x and of the weight.  Weights' gradients are summed over all tokens and heads in
- * a fixed order (that depends on sizes and the GPU's compute units alone) and rounded once; with any of them scratch_dev has
+ * a fixed order (that depends on sizes, on which of q and k there are and on the GPU's compute units alone) and rounded once; with any of them scratch_dev has
  * cb_norm_rotate_back_scratch_bytes, 16-byte aligned.  x_grad may be out_grad, with its strides, and overlaps no other tensor. */
 typedef struct {
     cb_heads x, out_grad, x_grad;
@@ -523,7 +523,7 @@ int cb_cache_bound(const cb_cache *cache, const int32_t *since_dev, void *hip_st
 
 /* Choose pages for one new token per sequence (row s of q: sequence s).  The score of a page is the largest, over the query heads that read the key
  * head, of sum_d max(q_d lo_d, q_d hi_d), which no product of q with a key of the page passes; summed in float64 and rounded to float32, and infinite where
- * it is not a number.  For every sequence and key head: the `first` first and the `recent` last of its pages, then those with the highest
+ * q or a bound is not a number (and where a bound is infinite).  n_seq * n_kv_heads * max_pages stays below 2^30.  For every sequence and key head: the `first` first and the `recent` last of its pages, then those with the highest
  * scores, ties to the lowest, `budget` in all or as many as there are.  chosen_dev (n_seq x n_kv_heads x budget) receives the pages' places in the
  * sequence's table, ascending, -1 behind them; count_dev (n_seq x n_kv_heads) how many.  Scores grow with the scale of an attention where that is positive. */
 typedef struct {

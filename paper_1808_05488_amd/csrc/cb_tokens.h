@@ -34,15 +34,19 @@ struct Cache {
 //   append:  counter 0: workgroups that have read the lengths
 //   attend:  counter ATTEND_COUNTERS + w: workgroups that have written their part of the (sequence, key head, block of query
 //            heads) whose first part is workgroup w's last one
+//   choose:  counter CHOOSE_COUNTERS + p: workgroups that have made their scores of (sequence, key head) p
 constexpr int ATTEND_ROWS = 16;            // query heads of a block
 constexpr int MAX_GROUPS = 1024;           // workgroups of the attention's launch at most
 constexpr int ATTEND_COUNTERS = 64;
-constexpr int COUNTER_BYTES = (ATTEND_COUNTERS + MAX_GROUPS) * 4;
+constexpr int CHOOSE_COUNTERS = ATTEND_COUNTERS + MAX_GROUPS;
+constexpr int CHOOSE_PAIRS = 4096;         // (sequence, key head) pairs that have a counter
+constexpr int COUNTER_BYTES = (CHOOSE_COUNTERS + CHOOSE_PAIRS) * 4;
 
 struct ScratchPlan {
     size_t parts, sums, scores, moves, pages, total;
 };
 ScratchPlan scratch_plan(const Cache& c, int q_heads);
+inline long rank_pitch(const Cache& c) { return (c.max_pages + 3L) / 4 * 4; }      // of the pages' ranks, read in fours
 
 struct RotaryJob {
     double turns[CB_ROTARY_MAX_PAIRS];
@@ -97,6 +101,7 @@ struct ChooseJob {
     int budget, first, recent;
     int32_t *chosen, *count;
 };
+bool choose_fits(const Cache& c);                   // its pages can be counted in 32 bits
 hipError_t launch_bound(const int32_t* since, const Cache& c, hipStream_t st);
 hipError_t launch_choose(const ChooseJob& j, const Cache& c, hipStream_t st);
 

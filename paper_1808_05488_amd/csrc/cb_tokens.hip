@@ -35,7 +35,7 @@ ScratchPlan scratch_plan(const Cache& c, int q_heads)
     p.scores = p.sums + (c.weight ? align256((size_t)c.seqs * q_heads * 8) : 0);
     const size_t attend = p.scores + (c.weight ? align256((size_t)c.seqs * q_heads * c.capacity * 4) : 0);
     const size_t evict = p.moves + (c.weight ? align256(pairs * (1 + 2 * (size_t)c.capacity) * 4) : 0);
-    const size_t choose = p.pages + (c.bounds ? align256(pairs * (size_t)c.max_pages * 4) : 0);
+    const size_t choose = p.pages + (c.bounds ? align256(pairs * (size_t)rank_pitch(c) * 4) : 0);
     p.total = attend > evict ? attend : evict;
     p.total = p.total > choose ? p.total : choose;
     return p;
@@ -353,7 +353,7 @@ int cb_cache_bound(const cb_cache* cache, const int32_t* since_dev, void* hip_st
 {
     cb::Cache c = {};
     CB_CHECKED(cb::check_cache(cache, true, 0, &c));
-    if (!c.bounds) return CB_EINVAL;
+    if (!c.bounds || !cb::choose_fits(c)) return CB_EINVAL;
     CB_LAUNCHED(cb::launch_bound(since_dev, c, (hipStream_t)hip_stream));
     return CB_OK;
 }
@@ -367,7 +367,7 @@ int cb_cache_choose(const cb_cache* cache, const cb_choose_params* params, const
     CB_CHECKED(cb::check_cache(cache, true, 0, &c));
     cb::ChooseJob j = {};
     CB_CHECKED(cb::check_heads(q, cb::values_dtype(*cache), &j.q, false));
-    if (!c.bounds || q->heads % c.heads) return CB_EINVAL;
+    if (!c.bounds || q->heads % c.heads || !cb::choose_fits(c)) return CB_EINVAL;
     j.budget = params->budget; j.first = params->first; j.recent = params->recent;
     j.chosen = chosen_dev; j.count = count_dev;
     CB_LAUNCHED(cb::launch_choose(j, c, (hipStream_t)hip_stream));
