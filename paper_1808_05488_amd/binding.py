@@ -748,6 +748,9 @@ class Rotary:
         self.head_dim, self.n_axes = head_dim, len(pairs)
         self.plan = cb_rotary()
         _check(lib().cb_rotary_init(C.byref(d), C.byref(self.plan)), "cb_rotary_init")
+        nbytes = C.c_size_t()
+        _check(lib().cb_norm_rotate_back_scratch_bytes(C.byref(self.plan), C.byref(nbytes)), "cb_norm_rotate_back_scratch_bytes")
+        self._back_bytes = nbytes.value
 
     def rotate(self, q: torch.Tensor, positions: torch.Tensor, k: Optional[torch.Tensor] = None, inverse: bool = False,
                q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
@@ -833,9 +836,7 @@ class Rotary:
             x_grad = torch.empty_like(x, memory_format=torch.contiguous_format) if of_x else None
             weight_grad = torch.empty_like(weight) if of_weight else None
             if of_weight and scratch is None:
-                nbytes = C.c_size_t()
-                _check(lib().cb_norm_rotate_back_scratch_bytes(C.byref(self.plan), C.byref(nbytes)), "cb_norm_rotate_back_scratch_bytes")
-                scratch = torch.empty(nbytes.value, dtype=torch.uint8, device=x.device)
+                scratch = torch.empty(self._back_bytes, dtype=torch.uint8, device=x.device)
             packed.append(_heads(x, "x", dtype, index, dim) + _heads(out_grad, "gradient", dtype, index, dim, x.shape[1], n) +
                           (_fresh(x_grad, dim) if of_x else _pack_heads(0, 0, 0, 0, 0)) +
                           _pack_two(weight.data_ptr(), weight_grad.data_ptr() if of_weight else 0))

@@ -28,18 +28,17 @@ __device__ __forceinline__ float scale_for(float top)
 }
 
 template <int VE> struct Codes { uint8_t e[VE]; };
-// VE values as codes, to the nearest, ties to even; beyond the largest the largest, what is not a number stays so
+// VE values, none above the largest that 8 bits hold, as codes: to the nearest, ties to even; what is not a number stays so
 template <int VE> __device__ __forceinline__ void encode(const float (&f)[VE], uint8_t* to)
 {
-    auto fit = [](float x) { return x == x ? __builtin_amdgcn_fmed3f(x, -MOST, MOST) : x; };
-    if constexpr (VE == 1) *to = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(fit(f[0]), 0.0f, 0, false);
-    else if constexpr (VE == 2) *reinterpret_cast<uint16_t*>(to) = (uint16_t)__builtin_amdgcn_cvt_pk_fp8_f32(fit(f[0]), fit(f[1]), 0, false);
+    if constexpr (VE == 1) *to = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[0], 0.0f, 0, false);
+    else if constexpr (VE == 2) *reinterpret_cast<uint16_t*>(to) = (uint16_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
     else {
         uint32_t w[VE / 4];
 #pragma unroll
         for (int i = 0; i < VE / 4; ++i) {
-            const int low = __builtin_amdgcn_cvt_pk_fp8_f32(fit(f[4 * i]), fit(f[4 * i + 1]), 0, false);
-            w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fit(f[4 * i + 2]), fit(f[4 * i + 3]), low, true);
+            const int low = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i], f[4 * i + 1], 0, false);
+            w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2], f[4 * i + 3], low, true);
         }
         if constexpr (VE == 4) *reinterpret_cast<uint32_t*>(to) = w[0];
         else *reinterpret_cast<uint64_t*>(to) = (uint64_t)w[1] << 32 | w[0];
@@ -55,6 +54,7 @@ template <typename T, int VE, int DP>
 __global__ __launch_bounds__(THREADS) void append_bytes_kernel(const RotaryJob j, const Cache c, int pieces, int lengths)
 {
     typedef Vec<T, VE> V;
+    typedef typename Word<sizeof(V)>::type W;
     constexpr int ITEMS = DP / (8 * VE);         // of a lane: (token, piece of its row), two vectors each
     extern __shared__ float2 cs[];               // BLOCK x pairs
     __shared__ int last;
@@ -118,68 +118,108 @@ __global__ __launch_bounds__(THREADS) void append_bytes_kernel(const RotaryJob j
         }
     if ((unsigned)page >= (unsigned)c.n_pages) return;
 
+    // where a lane's items lie: token and piece of its row
+    int token[ITEMS], piece[ITEMS];
+    bool is_new[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        token[i] = (lane + 64 * i) / pieces;
+        piece[i] = lane + 64 * i - token[i] * pieces;
+        is_new[i] = token[i] >= from && token[i] < to;
+    }
+    // rows of which nothing turns are taken by halves, where these are whole vectors: a load or store of the wavefront has whole lines then, not every
+    // other 16 bytes (45.7 -> 43.8 us)
+    const int half = c.dim % (2 * VE) == 0 ? c.dim / 2 : 0;
+    auto first_of = [&](bool key, int i) {
+        const bool turns = key && piece[i] < turned;
+        return (turns && !j.adjacent) || (!(key && np) && half) ? VE * piece[i] : 2 * VE * piece[i];
+    };
+    auto second_of = [&](bool key, int i) {
+        const bool turns = key && piece[i] < turned;
+        return !(key && np) && half ? half + VE * piece[i] : (turns && !j.adjacent ? np + VE * piece[i] : 2 * VE * piece[i] + VE);
+    };
+    W raw[ITEMS][2];
+    auto fetch = [&](int unit) {
+        const bool key = unit < c.heads;
+        const T* src = (const T*)(key ? j.k.data : j.v.data) + (long)(key ? unit : unit - c.heads) * (key ? j.k.head : j.v.head);
+        const long stride = key ? j.k.token : j.v.token;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const T* row = src + (token0 + token[i]) * stride;
+            auto get = [](bool there, const T* from) {
+                W v = W{};
+                if (there) v = *reinterpret_cast<const W*>(from);
+                return v;
+            };
+            raw[i][0] = get(is_new[i], row + first_of(key, i));
+            raw[i][1] = get(is_new[i] && second_of(key, i) < c.dim, row + second_of(key, i));
+        }
+    };
     for (int unit = blockIdx.y * WAVES + wave; unit < 2 * c.heads; unit += gridDim.y * WAVES) {
         const bool key = unit < c.heads;
         const int h = key ? unit : unit - c.heads;
-        const Heads& src = key ? j.k : j.v;
         const long head = (long)page * c.heads + h;
         uint8_t* dst = (uint8_t*)(key ? c.k : c.v) + ((head << c.page_shift) + (slot0 & ((1 << c.page_shift) - 1))) * c.dim;
         float* scale_at = (key ? c.k_scale : c.v_scale) + (head << (c.page_shift - 4)) + ((slot0 & ((1 << c.page_shift) - 1)) >> 4);
         const float old = from > 0 ? *scale_at : 0.0f;
+        fetch(unit);
         float f[ITEMS][2][VE];
-        int token[ITEMS], first[ITEMS], second[ITEMS];
         float top = 0.0f;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int it = lane + 64 * i, t = it / pieces, piece = it - t * pieces;
-            const bool turns = key && piece < turned;
-            token[i] = t;
-            first[i] = turns && !j.adjacent ? VE * piece : 2 * VE * piece;
-            second[i] = turns && !j.adjacent ? np + VE * piece : 2 * VE * piece + VE;
-            V a = {}, b = {};
-            if (t >= from && t < to) {
-                const T* row = (const T*)src.data + (token0 + t) * src.token + (long)h * src.head;
-                a = load_once<true, V>(row + first[i]);
-                if (second[i] < c.dim) b = load_once<true, V>(row + second[i]);
-            }
+            const V a = __builtin_bit_cast(V, raw[i][0]), b = __builtin_bit_cast(V, raw[i][1]);
 #pragma unroll
             for (int e = 0; e < VE; ++e) { f[i][0][e] = widen(a.e[e]); f[i][1][e] = widen(b.e[e]); }
         }
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int it = lane + 64 * i, t = it / pieces, piece = it - t * pieces;
-            if (key && piece < turned && t >= from && t < to) turn<VE>(cs + t * np + piece * VE, j.adjacent, f[i][0], f[i][1]);
+            if (key && piece[i] < turned && is_new[i]) turn<VE>(cs + token[i] * np + piece[i] * VE, j.adjacent, f[i][0], f[i][1]);
 #pragma unroll
-            for (int e = 0; e < VE; ++e)
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const float size = fabsf(f[i][x][e]);
-                    top = fmaxf(top, size < __builtin_inff() ? size : 0.0f);
-                }
+            for (int e = 0; e < VE; ++e) top = fmaxf(top, fmaxf(fabsf(f[i][0][e]), fabsf(f[i][1][e])));      // (what is not a number is passed over)
         }
-        const float need = scale_for(wave_max(top)), now = from > 0 ? fmaxf(need, old) : need;
+        top = wave_max(top);
+        const bool infinite = top == __builtin_inff();
+        if (infinite) {
+            top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+                for (int e = 0; e < VE; ++e)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const float size = fabsf(f[i][x][e]);
+                        top = fmaxf(top, size < __builtin_inff() ? size : 0.0f);
+                    }
+            top = wave_max(top);
+        }
+        const float need = scale_for(top), now = from > 0 ? fmaxf(need, old) : need;
         const uint32_t bits = __float_as_uint(now);
         const bool exact = (bits & 0x7FFFFFu) == 0 && bits >= 0x00800000u && bits <= 0x7E000000u;      // 2^-126 .. 2^125: so is its inverse
         const float inverse = exact ? __uint_as_float(0x7F000000u - bits) : 0.0f;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int t = token[i];
-            uint8_t* row = dst + (long)t * c.dim;
-            if (t < from && now != old) {
+            const int first = first_of(key, i), second = second_of(key, i);
+            uint8_t* row = dst + (long)token[i] * c.dim;
+            if (token[i] < from && now != old) {
                 const float ratio = old / now;
-                decode<VE>(row + first[i], f[i][0]);
-                if (second[i] < c.dim) decode<VE>(row + second[i], f[i][1]);
+                decode<VE>(row + first, f[i][0]);
+                if (second < c.dim) decode<VE>(row + second, f[i][1]);
 #pragma unroll
                 for (int e = 0; e < VE; ++e) { f[i][0][e] *= ratio; f[i][1][e] *= ratio; }
-            } else if (t >= from && t < to) {
+            } else if (is_new[i]) {
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
                     f[i][0][e] = exact ? f[i][0][e] * inverse : f[i][0][e] / now;
                     f[i][1][e] = exact ? f[i][1][e] * inverse : f[i][1][e] / now;
                 }
+                if (infinite)
+#pragma unroll
+                    for (int e = 0; e < VE; ++e)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) f[i][x][e] = f[i][x][e] == f[i][x][e] ? __builtin_amdgcn_fmed3f(f[i][x][e], -MOST, MOST) : f[i][x][e];
             } else continue;
-            encode<VE>(f[i][0], row + first[i]);
-            if (second[i] < c.dim) encode<VE>(f[i][1], row + second[i]);
+            encode<VE>(f[i][0], row + first);
+            if (second < c.dim) encode<VE>(f[i][1], row + second);
         }
         if (lane == 0) *scale_at = now;
     }
@@ -201,10 +241,10 @@ hipError_t launch_append_bytes(const RotaryJob& j, const Cache& c, int* lengths,
 {
     const int ve = vector_values<2>(j.bf16, j.pairs, {&j.k, &j.v}), pieces = (c.dim + 2 * ve - 1) / (2 * ve);
     const long blocks = j.offsets ? j.tokens / BLOCK + 2L * c.seqs : c.seqs;
-    // a wavefront a head where there are few blocks, up to eight heads where there are many
+    // a wavefront a head where there are few blocks, two heads where there are many (42 us with four or eight)
     const int units = 2 * c.heads, most = (units + WAVES - 1) / WAVES;
     int split = most;
-    while (split > 1 && blocks * (split / 2) >= 4L * device_units() && most / (split / 2) <= 8) split /= 2;
+    while (split > 1 && blocks * (split / 2) >= 4L * device_units() && most / (split / 2) <= 2) split /= 2;
     const dim3 grid((unsigned)blocks, (unsigned)split);
     if (*lengths == LENGTHS_LAST && blocks * split > 64) *lengths = LENGTHS_LATER;
     if (j.bf16) {

@@ -98,10 +98,15 @@ template <bool CHOSEN> struct Tiles {
     int seqs, capacity, per_seq;       // per_seq: (key head, block) pairs of a sequence
     int tokens, enough;                // of a tile; tiles of a pair that keep a workgroup busy
     int page_shift, budget;
+    int known;                         // up to 64 sequences: the length of a lane's
+    __device__ void read() { known = seqs <= 64 && (int)(threadIdx.x & 63) < seqs ? clamp_length(lengths[threadIdx.x & 63], capacity) : 0; }
+    // the length of a sequence, of each lane's or of one for all
+    __device__ int real_of_lane(int seq) const { return seqs <= 64 ? known : clamp_length(lengths[seq], capacity); }
+    __device__ int real(int seq) const { return seqs <= 64 ? __builtin_amdgcn_readlane(known, seq) : clamp_length(lengths[seq], capacity); }
+    __device__ int length(int seq) const { return gone_through(real(seq)); }
     // tokens of a sequence that are gone through: those of chosen pages are counted one page behind the other, whole ones
-    __device__ int length(int seq) const
+    __device__ int gone_through(int len) const
     {
-        const int len = clamp_length(lengths[seq], capacity);
         if constexpr (!CHOSEN) return len;
         const int pages = (len + (1 << page_shift) - 1) >> page_shift;
         return (pages < budget ? pages : budget) << page_shift;
@@ -118,7 +123,7 @@ template <bool CHOSEN> struct Tiles {
         const int lane = threadIdx.x & 63;
         int sum = 0, all = 0;
         for (int s = lane; s < seqs; s += 64) {
-            const int n = of(length(s));
+            const int n = of(gone_through(real_of_lane(s)));
             sum += n;
             all += worth(n);
         }
@@ -131,7 +136,7 @@ template <bool CHOSEN> struct Tiles {
         const int lane = threadIdx.x & 63;
         int before = 0;
         for (int s0 = 0; s0 < seqs; s0 += 64) {
-            const int n = s0 + lane < seqs ? of(length(s0 + lane)) : 0;
+            const int n = s0 + lane < seqs ? of(gone_through(real_of_lane(s0 + lane))) : 0;
             const int sum = wave_scan((by_worth && n ? worth(n) : n) * per_seq);
             const unsigned long long past = __ballot(before + sum > u);
             if (past) {
@@ -192,9 +197,9 @@ template <int SUB> __device__ __forceinline__ Pages load_chosen(const int32_t* t
 {
     const int lane = threadIdx.x & 63, tok = ((tile + lane / SUB * step) * SUB + lane % SUB) * 16, at = tok >> shift;
     int page = -1, left = 0;
-    if (tok < len && at < count) {
+    if (tok < len) {                   // (the list goes that far, whatever its count is, which is on its way beside it)
         const int p = chosen[at];
-        if ((unsigned)p < (unsigned)max_pages) {
+        if (at < count && (unsigned)p < (unsigned)max_pages) {
             left = real - ((p << shift) + (tok & ((1 << shift) - 1)));
             if (left > 0) page = table[p];
         }
@@ -258,7 +263,8 @@ __global__ __launch_bounds__((Tile<KT, T, DP>::WAVES * 64)) void attend_kernel(c
     const Cache& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
     const int D = c.dim, per_seq = c.heads * a.blocks;
-    const Tiles<CHOSEN> tiles{c.lengths, c.seqs, c.capacity, per_seq, TL::TOKENS, SPLIT_TILES * WAVES, c.page_shift, a.budget};
+    Tiles<CHOSEN> tiles{c.lengths, c.seqs, c.capacity, per_seq, TL::TOKENS, SPLIT_TILES * WAVES, c.page_shift, a.budget, 0};
+    tiles.read();
     unsigned total, groups;
     tiles.total(&total, &groups);
     const bool own_group = groups <= gridDim.x;                        // of a pair
@@ -308,7 +314,7 @@ __global__ __launch_bounds__((Tile<KT, T, DP>::WAVES * 64)) void attend_kernel(c
         x.row0 = (x.pair - x.h * a.blocks) * ROWS;
         x.rows = a.group - x.row0 < ROWS ? a.group - x.row0 : ROWS;
         if constexpr (CHOSEN) {
-            x.real = clamp_length(c.lengths[seq], c.capacity);
+            x.real = tiles.real(seq);
             x.count = a.count[(long)seq * c.heads + x.h];
         }
         return x;
@@ -752,15 +758,20 @@ __global__ __launch_bounds__((Tile<KT, T, DP>::WAVES * 64)) void attend_kernel(c
             *y += f * v[p].y;
         }
     };
-    bool mine[2] = {false, false};                             // parts of this workgroup that others have to do with
     // (a part that begins before its wavefront's run belongs to the chain of an earlier one, but for the workgroup's first)
     const unsigned long long heads = __ballot(lane < 2 * WAVES && of_slot.x >= 0 && (lane == 0 || (lane & 1)));
-    for (unsigned long long rest = heads; rest; rest &= rest - 1) {
+    // chains are worked through side by side, as many wavefronts a chain as there are for it (one after the other 8 chains took 5 us)
+    const int chains = __builtin_popcountll(heads);
+    int own_waves = WAVES;
+    while (own_waves > 1 && own_waves * chains > WAVES) own_waves /= 2;
+    unsigned long long rest = heads;
+    for (int at = wave / own_waves; at < chains; at += WAVES / own_waves) {
+        // the at-th one: as many bits as lie between are taken off
+        for (int k = chains - __builtin_popcountll(rest); k < at; ++k) rest &= rest - 1;
         const Chain x = chain(__builtin_ctzll(rest));
         const bool whole = x.first >= run && x.first + x.n <= run_end;
-        const int w = x.first < run ? 0 : 1;
-        float* to = a.parts + (2L * blockIdx.x + w) * part_floats<DP>();
-        for (int i = 2 * tid; i < x.rows * DP; i += 2 * THREADS) {
+        float* to = a.parts + (2L * blockIdx.x + (x.first < run ? 0 : 1)) * part_floats<DP>();
+        for (int i = 2 * (tid - wave / own_waves * own_waves * 64); i < x.rows * DP; i += 2 * own_waves * 64) {
             const int row = i / DP, d = i % DP;
             float M, L, y, z;
             join(x.slot, x.wave, x.parts, row, d, &M, &L, &y, &z);
@@ -770,8 +781,10 @@ __global__ __launch_bounds__((Tile<KT, T, DP>::WAVES * 64)) void attend_kernel(c
                 if (d == 0) put(to + 2 * row, M, L);
             }
         }
-        if (!whole) mine[w] = true;
     }
+    // parts of this workgroup that others have to do with
+    const bool shared = lane < 2 * WAVES && (heads >> lane & 1) && (of_slot.x < run || of_slot.x + of_slot.w > run_end);
+    const bool mine[2] = {__ballot(shared && of_slot.x < run) != 0, __ballot(shared && of_slot.x >= run) != 0};
     if (!mine[0] && !mine[1]) return;
     __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): this wavefront's stores are where every compute unit sees them
     __syncthreads();
