@@ -365,7 +365,9 @@ __global__ __launch_bounds__(THREADS) void choose_kernel(const ChooseArgs a)
         int want = budget - (a.j.first + a.j.recent);
         bool found = want == 0;
         if (found) low = high = ALWAYS - 1;
-        for (int turn = 0; !found; turn ^= 1) {
+        // (ten bits a pass: four at most, whatever the ranks are)
+        for (int pass = 0; pass < 4 && !found; ++pass) {
+            const int turn = pass & 1;
             const int bits = 32 - __builtin_clz((high - low) | 1u), shift = bits > DIGIT ? bits - DIGIT : 0;
             each([&](uint32_t k) {
                 if (k >= low && k <= high) atomicAdd(&hist[(k - low) >> shift], 1);
@@ -415,11 +417,11 @@ __global__ __launch_bounds__(THREADS) void choose_kernel(const ChooseArgs a)
                 for (int x = 0; x < 4; ++x) {
                     const uint32_t k = r[i][x];
                     const int p = base + 4 * (tid + THREADS * i) + x;
-                    if (k > high) chosen[sure++ + (equal < want ? equal : want)] = p;
-                    else if (k >= low) {
-                        if (equal < want) chosen[sure + equal] = p;
-                        ++equal;
-                    }
+                    const bool tie = k >= low && k <= high;
+                    const int to = sure + (equal < want ? equal : want);
+                    if ((k > high || (tie && equal < want)) && to < budget) chosen[to] = p;
+                    sure += k > high;
+                    equal += tie;
                 }
             }
         }

@@ -437,7 +437,7 @@ int pool_mask(const cb_pool* p)
 
 extern "C" {
 
-int cb_version(void) { return 100; }
+int cb_version(void) { return 200; }
 
 int cb_last_hip_error(void) { return g_last_hip; }
 

@@ -230,6 +230,28 @@ def test_gradients_of_gradients_of_the_norm_are_refused():
         torch.autograd.grad(g.sum(), x)
 
 
+def test_gradients_of_shared_and_broadcast_inputs():
+    """One weight for queries and keys, queries that are one token's repeated, the same tensor as queries and keys."""
+    rng = np.random.default_rng(14)
+    n, heads, dim, pairs = 40, 3, 32, (4, 6, 6)
+    pos, rot = rng.integers(0, 99, (n, 3)).astype(np.int32), cb.Rotary(32, (4, 6, 6))
+    one, w = dev(rng.standard_normal((1, heads, dim)), F32).requires_grad_(), dev(rng.standard_normal(dim), F32).requires_grad_()
+    gq, gk = (dev(rng.standard_normal((n, heads, dim)), F32) for _ in range(2))
+    x = one.expand(n, heads, dim)
+    q, k = rot.norm_rotate(x, dev(pos), w, k=x, k_weight=w)
+    g_one, g_w = torch.autograd.grad((q, k), (one, w), (gq, gk))
+    want_x, want_w, spread_x, spread_w = 0.0, 0.0, 0.0, 0.0
+    for g in (gq, gk):
+        a, b, norms, r = norm_back64(f64(x), f64(w), f64(g), pos, pairs, 0, 0, 1e-6)
+        size, wabs = turned_size(f64(g), pairs, 0), np.abs(f64(w))
+        want_x, want_w = want_x + a, want_w + b
+        spread_x = spread_x + r * (wabs * size + np.abs(norms) * (wabs * size * np.abs(norms)).mean(2, keepdims=True))
+        spread_w = spread_w + (size * np.abs(norms)).sum((0, 1))
+    # (every term as in check_back, and sums of 80 of them: 80 units more at most)
+    within(f64(g_one), want_x.sum(0, keepdims=True), (176 * EPS + ANGLE) * spread_x.sum(0, keepdims=True), "gradient of one token's")
+    within(f64(g_w), want_w, (400 * EPS + ANGLE) * spread_w, "gradient of the weight")
+
+
 def test_norm_of_nothing():
     rot, pos = cb.Rotary(16, (8,)), torch.empty((0, 1), dtype=torch.int32, device="cuda")
     q, w = torch.empty((0, 3, 16), device="cuda", requires_grad=True), torch.ones(16, device="cuda", requires_grad=True)
@@ -791,6 +813,39 @@ def test_choose_ties_go_to_the_lowest(values):
     for budget, first, recent in ((7, 0, 0), (100, 3, 4), (300, 10, 0), (5, 2, 3), (pages, 0, 0), (pages - 1, 0, 0)):
         for sign in (1.0, -1.0, 0.0):
             check_choose(c, torch.full((1, 2, dim), sign, device="cuda"), [n], budget, first, recent)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("seqs,heads", [(70, 3), (700, 8)])
+def test_choose_of_many_sequences(kind, seqs, heads):
+    """More sequences than a wavefront has lanes, more (sequence, key head) pairs than there are counters; sequences read the same pages."""
+    rng = np.random.default_rng([seqs, heads])
+    pages, page, dim = 300, 16, 16
+    lengths = rng.integers(0, pages * page + 1, seqs)
+    lengths[:5] = [0, 1, 16 * 20, 16 * 20 + 1, pages * page]
+    one = make_bytes(rng, [pages * page], heads, dim, page) if kind == "e4m3" else make_cache(rng, [pages * page], heads, dim, page, F32 if kind == "f32" else BF16, evictable=False)
+    dtype = one.bounds.dtype if one.bounds is not None else (BF16 if kind == "e4m3" else one.dtype)
+    bounds = torch.sort(dev(rng.standard_normal((one.k_pages.shape[0], heads, 2, dim)), dtype), 2).values
+    tables = np.stack([one.table.cpu().numpy()[0][rng.permutation(pages)] for _ in range(seqs)])
+    c = cb.TokenCache(one.k_pages, one.v_pages, dev(tables), dev(lengths.astype(np.int32)), k_scale=one.k_scale, v_scale=one.v_scale, bounds=bounds)
+    q = dev(rng.standard_normal((seqs, 2 * heads, dim)), F32 if kind == "f32" else BF16)
+    pick = check_choose(c, q, lengths.tolist(), 20, 1, 2)
+    if seqs < 100:
+        check_chosen(c, q, lengths.tolist(), pick)
+        want = [c.attend(q)[0][s] for s in (3, 4, 69)]
+        small = cb.TokenCache(one.k_pages, one.v_pages, dev(tables[[3, 4, 69]]), dev(lengths[[3, 4, 69]].astype(np.int32)), k_scale=one.k_scale, v_scale=one.v_scale)
+        got = small.attend(q[[3, 4, 69]].contiguous())[0]
+        within(f64(got), f64(torch.stack(want)), 64 * EPS + 2 * ROUND[q.dtype] * np.abs(f64(got)), "the same sequences among others")
+        since = dev(np.maximum(lengths - 30, 0).astype(np.int32))
+        alone = cb.TokenCache(one.k_pages, one.v_pages, dev(one.table.cpu().numpy()), dev(np.array([pages * page], np.int32)), k_scale=one.k_scale, v_scale=one.v_scale, bounds=torch.zeros_like(bounds))
+        alone.bound()
+        full = dev(np.full(seqs, pages * page, np.int32))
+        c.lengths.copy_(full)                                    # (whole pages: whichever sequence writes a page's bounds writes the same)
+        c.bound(torch.minimum(since, full))
+        touched = torch.zeros(bounds.shape[0], dtype=torch.bool)
+        for s in range(seqs):
+            touched[tables[s, int(since[s]) // page:]] = True
+        assert torch.equal(c.bounds.cpu()[touched], alone.bounds.cpu()[touched])
 
 
 def test_choose_scores_far_apart_and_without_pages():
