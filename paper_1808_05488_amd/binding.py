@@ -656,6 +656,7 @@ _pack_choose = struct.Struct("@iiii").pack
 assert struct.calcsize("@Pqqii") == C.sizeof(cb_heads) and struct.calcsize("@fffii") == C.sizeof(cb_attend_params)
 assert struct.calcsize("@iiPPP") == C.sizeof(cb_evict_params) and struct.calcsize("@iiii") == C.sizeof(cb_choose_params)
 assert 3 * struct.calcsize("@Pqqii") + 2 * struct.calcsize("@P") == C.sizeof(cb_norm_back)
+_NO_HEADS = _pack_heads(0, 0, 0, 0, 0)
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -726,12 +727,17 @@ class _NormRotation(torch.autograd.Function):
         return q_out, k_out
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, q_grad, k_grad):
+    def _gradients(ctx, q_grad, k_grad):
         positions, q, q_weight, k, k_weight = ctx.saved_tensors
         need = ctx.needs_input_grad
-        back = ctx.rotary._norm_back(positions, ctx.eps, (q, q_weight, q_grad, need[3], need[4]), (k, k_weight, k_grad, need[5], need[6]))
-        return (None, None, None) + back
+        return (None, None, None) + ctx.rotary._norm_back(positions, ctx.eps, (q, q_weight, q_grad, need[3], need[4]), (k, k_weight, k_grad, need[5], need[6]))
+
+    # (what refuses gradients of gradients takes 4 us of the host's time: only where there may be some)
+    _gradients_once = staticmethod(torch.autograd.function.once_differentiable(_gradients.__func__))
+
+    @staticmethod
+    def backward(ctx, q_grad, k_grad):
+        return (_NormRotation._gradients_once if torch.is_grad_enabled() else _NormRotation._gradients)(ctx, q_grad, k_grad)
 
 
 class Rotary:
@@ -824,26 +830,30 @@ class Rotary:
 
     def _norm_back(self, positions, eps, *sides):
         """Gradients of (x, weight) of each side: (x, weight, gradient of the output or None, whether x's is wanted, the weight's)."""
+        # (this runs in a thread of its own, where every step takes longer than elsewhere)
         grads, packed, scratch = [], [], None
-        dim, index, wdtype = self.head_dim, positions.get_device(), sides[0][1].dtype
-        n, dtype = sides[0][0].shape[0], sides[0][0].dtype
+        dim, index, first, weight = self.head_dim, positions.get_device(), sides[0][0], sides[0][1]
+        n, dtype, wdtype = first.shape[0], first.dtype, weight.dtype
         for x, weight, out_grad, of_x, of_weight in sides:
             if x is None or out_grad is None or not (of_x or of_weight):
-                grads += [None, None]
+                grads += (None, None)
                 packed.append(None)
                 continue
-            out_grad = out_grad.contiguous()                     # (a gradient comes in any strides)
-            x_grad = torch.empty_like(x, memory_format=torch.contiguous_format) if of_x else None
-            weight_grad = torch.empty_like(weight) if of_weight else None
-            if of_weight and scratch is None:
-                scratch = torch.empty(self._back_bytes, dtype=torch.uint8, device=x.device)
+            if not out_grad.is_contiguous():                     # (a gradient comes in any strides)
+                out_grad = out_grad.contiguous()
+            x_grad = weight_grad = None
+            if of_x:
+                x_grad = torch.empty_like(x, memory_format=torch.contiguous_format)
+            if of_weight:
+                weight_grad = torch.empty_like(weight)
+                if scratch is None:
+                    scratch = positions.new_empty(self._back_bytes // 4)
             packed.append(_heads(x, "x", dtype, index, dim) + _heads(out_grad, "gradient", dtype, index, dim, x.shape[1], n) +
-                          (_fresh(x_grad, dim) if of_x else _pack_heads(0, 0, 0, 0, 0)) +
-                          _pack_two(weight.data_ptr(), weight_grad.data_ptr() if of_weight else 0))
-            grads += [x_grad, weight_grad]
+                          (_fresh(x_grad, dim) if of_x else _NO_HEADS) + _pack_two(weight.data_ptr(), weight_grad.data_ptr() if of_weight else 0))
+            grads += (x_grad, weight_grad)
         if any(p is not None for p in packed):
             status = lib().cb_norm_rotate_back(C.byref(self.plan), _CB_DT[dtype], n, positions.data_ptr(), eps, _CB_DT[wdtype], packed[0], packed[1],
-                                               None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel(), _raw_stream(index))
+                                               None if scratch is None else scratch.data_ptr(), self._back_bytes, _raw_stream(index))
             if status:
                 _check(status, "cb_norm_rotate_back")
         return tuple(grads)
