@@ -6,7 +6,8 @@
 // (A scale that a caller has written may be any number: the values are divided by it then.)
 //
 // A block and a head belong to one wavefront: it reads the new tokens' rows, turns keys, takes the maximum across its lanes from registers,
-// and writes 16 rows of a page that lie one behind the other.  Memory bounds it: 2 or 4 bytes read and 1 written a value.
+// and writes 16 rows of a page that lie one behind the other.  Memory bounds it: 2 or 4 bytes read and 1 written a value (35 000 tokens of 8 heads of 128 in
+// bfloat16: 40 us, 5.4 TB/s).  One token for each of 16 sequences takes 3.8 us, trips to memory one behind the other: start, page, rows and the scale that is there.
 // A workgroup has one block of tokens, whose angles it makes once, and some or all of its heads.  Which block of which sequence the device finds
 // itself: sequence s has the numbers from offsets[s] / 16 + 2 s on, which leaves room for one begun block in front and one behind.
 #include "cb_rows.h"

@@ -3,7 +3,7 @@
 // For each sequence and key head: s_j = scale q.k_j for the query heads that read the key head, the softmax over the
 // cached tokens j, and the weighted sum of the v_j.  Keys and values are read once, so memory bounds it: 4 * dim * heads operations for
 // 2 * dim * heads / group values (200 003 tokens of 8 key heads, 128 values in bfloat16: 131 us, 6.3 TB/s, where plain reads reach 7.2; 6.6 over
-// 32 x 8 192 tokens).  More than 16 query heads a key head are blocks of 16, and every block reads the keys and values again.
+// 32 x 8 192 tokens).  A cache in 8 bits has half the bytes (200 003 tokens: 80 us, of which 64 are at 6.5 TB/s and the rest the way to the first tile and the join).  More than 16 query heads a key head are blocks of 16, and every block reads the keys and values again.
 // One pass: every wavefront takes tiles of consecutive tokens and keeps, for up to 16 query heads, the running maximum m, the sum l of e^(s - m) and the sum o of e^(s - m) v (times a power of two, see Tiles::bits); a tile with a larger maximum scales l and o by e^(m - m').
 // Parts of a sequence (wavefronts of a workgroup, then workgroups) are joined the same way.
 //
@@ -11,6 +11,11 @@
 // that m and l live in the lane that needs them, and what S^T leaves in a lane -- the scores of tokens 4 * (lane >> 4) + r -- is
 // what P^T wants there, if the tokens of a tile are numbered to suit; no value changes lanes but for the maximum.  Keys and values come
 // from memory into registers as the matrix cores take them, whole rows by neighbouring lanes.
+//
+// 8 bits.  e4m3 values become bfloat16 in registers, exactly; the 16 tokens that share a scale are the 16 rows of S^T that a matrix instruction makes, so
+// that K's scale is one factor for all of them behind the product, and V's goes into P before it.  A float32 query is three bfloat16 terms.  Tiles of 64 tokens
+// instead of 32 make no difference.
+// Chosen pages.  The list's pages are gone through as if they lay one behind the other; a lane finds the page of a sub-tile and how many of its tokens there are.
 //
 // Work is split over the length, whatever the lengths, which the kernel reads itself.  Where there are workgroups enough, every pair (sequence,
 // key head, block of query heads) has its own, more of them the longer it is; where there are not, the tiles of all pairs, in order, are dealt to
@@ -56,7 +61,9 @@ constexpr float LOWEST = -3.402823466e38f;       // of a maximum, so that nothin
 constexpr int ROWS = ATTEND_ROWS;
 // Tiles of a wavefront that are worth a workgroup of their own: a part more costs its way through memory and the join.  (Measured for five sequences of
 // 1 - 9 001 tokens, float32 and 80 values a head: 25.8 us with 1, 22.6 with 2, 28.4 with 4.  Other head sizes and bfloat16 were not.)
-constexpr int SPLIT_TILES = 2;
+// Chosen pages are few: 64 of 64 tokens for each of 8 key heads take 17.5 us with 1 and 20.2 with 2 in bfloat16, 512 tokens for each of 8 in float32 13.6 and 12.8
+// (whose tiles are half as long, and take longer to compute than to load).
+template <typename KT, bool CHOSEN> constexpr int split_tiles() { return CHOSEN && sizeof(KT) < 4 ? 1 : 2; }
 
 // e^x for the difference x of two scores, which is exact or nearly so; scores times log2 e would be rounded at their own size.  What the product is
 // rounded by, and what log2 e is, come in as a factor 1 + rest: without it e^-80 would be off by 2e-6 of itself (and five sequences of 1 - 9 001 tokens in
@@ -263,7 +270,7 @@ __global__ __launch_bounds__((Tile<KT, T, DP>::WAVES * 64)) void attend_kernel(c
     const Cache& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
     const int D = c.dim, per_seq = c.heads * a.blocks;
-    Tiles<CHOSEN> tiles{c.lengths, c.seqs, c.capacity, per_seq, TL::TOKENS, SPLIT_TILES * WAVES, c.page_shift, a.budget, 0};
+    Tiles<CHOSEN> tiles{c.lengths, c.seqs, c.capacity, per_seq, TL::TOKENS, split_tiles<KT, CHOSEN>() * WAVES, c.page_shift, a.budget, 0};
     tiles.read();
     unsigned total, groups;
     tiles.total(&total, &groups);

@@ -2,7 +2,8 @@
 //
 // Bounds.  For a page and key head the smallest and the largest of its tokens' keys, value by value.  Only pages with new tokens are gone through;
 // memory bounds it (their keys).  A workgroup takes a page and a head, its wavefronts some of the rows, a lane 4 - 16 bytes of a row.  A cache in 8 bits
-// has bounds in bfloat16, rounded outwards where its scales are no powers of two.
+// has bounds in bfloat16, rounded outwards where its scales are no powers of two.  (24 streams with 300 new tokens each, 8 heads of 128 in 8 bits: 6 us; with
+// sums over rows in LDS 21.)
 //
 // Scores.  sum_d max(q_d lo_d, q_d hi_d) is no less than q.k for any key k of the page; a page's score is the largest of its key head's query heads.  Sums
 // are in float64 and rounded to float32 once, so that what is chosen does not depend on their order (products of float32 values are exact there):
@@ -11,7 +12,8 @@
 //
 // Choice.  The workgroup that comes last of those that have made a (sequence, key head)'s scores finds the lowest score that is taken by counting digits
 // (radix selection, ten bits a pass between the lowest and the highest score), then lists the pages in order.  Sequences whose pages are all taken
-// need no scores.
+// need no scores.  3 126 pages of 8 key heads with 4 query heads each: 13 us, of which 3 are the way to the bounds, 3.6 the
+// scores, 2 until all workgroups have arrived, 4.5 the choice: steps that follow from each other.  (A launch of its own for the choice, by 1 024 threads: 16 us.)
 #include <type_traits>
 
 #include "cb_tokens.h"

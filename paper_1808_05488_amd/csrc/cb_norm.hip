@@ -4,11 +4,15 @@
 // position (cb_rotary.hip).  Backward, with g = R^-1(gradient of out): the gradient of x is r (w g - n mean(w g n)), that of w the sum over tokens and
 // heads of g n.  Since mean(w g n) = r mean(w g x), both sums over a head are made in one go.
 //
-// Heads are independent and read once, so memory bounds it: 2 values' bytes forward, 3 backward.  A head lies in the registers of 1 - 64 lanes (two
+// Heads are independent and read once, so memory bounds it: 2 values' bytes forward, 3 backward.  38 400 tokens x 40 heads of 128 in bfloat16 take 130 us (6.0
+// TB/s, reads and writes; a copy around the caches reaches 6.4), the gradients of 19 200 such tokens 120 us (4.9 TB/s: two wavefronts a SIMD with all that they hold, and
+// no more registers for a third) and 5 for the sums of the weights'.  A head lies in the registers of 1 - 64 lanes (two
 // vectors of 16 bytes a lane, as pairs need them), its sums take a few steps across them.  A wavefront goes through all heads of its tokens by itself: the
-// angles, which it makes once, the weights and all that addresses need stay in its registers.
+// angles, which it makes once, and all that addresses need stay in its registers.  (With a workgroup for a token, its angles in LDS and a division for every head the
+// clip took 208 us.)
 // A gradient of the weights is summed in registers by persistent workgroups, each of which leaves one row of sums; a second launch adds these
-// up in order, so that results do not vary.
+// up in order, so that results do not vary.  (The next heads' loads before this one's arithmetic: 13 us more.  Queries and keys, and heads that are
+// scaled, in code of their own, 24 KB instead of 16: 6 us more.)
 #include <climits>
 #include <type_traits>
 
@@ -154,12 +158,11 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
                 for (int e = 0; e < VE; ++e) at[p][e] = turns[p] ? s_cs[token * np + (sub + (p << log)) * VE + e] : make_float2(1.0f, 0.0f);
             __builtin_amdgcn_wave_barrier();
         }
-        auto take = [&](int u, int step, auto side_is) {
-            constexpr int side = side_is.value;
+        auto take = [&](int u, int step) {
+            const bool side = step >= sh.q_steps;                    // keys
             const int h = head0 + ((side ? step - sh.q_steps : step) << sh.heads_log);
             const bool there = real && h < (side ? j.k.heads : j.q.heads);
             float f[PPL][2][VE], d[PPL][2][VE], w[PPL][2][VE];       // the head; BACK: its gradient, turned back; the weights
-            float squares = 0.0f, dot = 0.0f;
 #pragma unroll
             for (int p = 0; p < PPL; ++p) {
                 const V xa = __builtin_bit_cast(V, x[u][p][0]), xb = __builtin_bit_cast(V, x[u][p][1]);
@@ -175,44 +178,45 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
                         d[p][0][e] = widen(ga.e[e]);
                         d[p][1][e] = widen(gb.e[e]);
                     }
-                    squares = __builtin_fmaf(f[p][0][e], f[p][0][e], squares);
-                    squares = __builtin_fmaf(f[p][1][e], f[p][1][e], squares);
                 }
-                if constexpr (BACK) {
-                    turn_by<VE, ADJACENT>(at[p], d[p][0], d[p][1]);
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) {
-                        dot = __builtin_fmaf(w[p][0][e] * d[p][0][e], f[p][0][e], dot);
-                        dot = __builtin_fmaf(w[p][1][e] * d[p][1][e], f[p][1][e], dot);
-                    }
-                }
+                if constexpr (BACK) turn_by<VE, ADJACENT>(at[p], d[p][0], d[p][1]);
             }
-            squares = head_sum(squares, log);
-            if constexpr (BACK) dot = head_sum(dot, log);
-            float mean = __builtin_fmaf(squares, scale, n.eps);
+            float mean, dot;
             int down = 0;                                            // f is the head times 2^-down
-            if (!(mean >= SMALL && mean <= LARGE)) {
-                float top = 0.0f;
+            // (once, or once more for a head that has been scaled: a loop, since a kernel's instructions come from memory too)
+#pragma unroll 1
+            for (bool again = false;; again = true) {
+                float squares = 0.0f;
+                dot = 0.0f;
 #pragma unroll
                 for (int p = 0; p < PPL; ++p)
 #pragma unroll
-                    for (int e = 0; e < VE; ++e) top = fmaxf(top, fmaxf(fabsf(f[p][0][e]), fabsf(f[p][1][e])));
-                const int e0 = exponent(head_max(top, log)), e1 = n.eps > 0.0f ? exponent(n.eps) / 2 : -127;
-                down = e0 > e1 ? e0 : e1;
-                squares = dot = 0.0f;
+                    for (int e = 0; e < VE; ++e)
 #pragma unroll
-                for (int p = 0; p < PPL; ++p)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int e = 0; e < VE; ++e) {
-                            f[p][i][e] = __builtin_ldexpf(f[p][i][e], -down);
+                        for (int i = 0; i < 2; ++i) {
                             squares = __builtin_fmaf(f[p][i][e], f[p][i][e], squares);
                             if constexpr (BACK) dot = __builtin_fmaf(w[p][i][e] * d[p][i][e], f[p][i][e], dot);
                         }
                 squares = head_sum(squares, log);
                 if constexpr (BACK) dot = head_sum(dot, log);
-                mean = __builtin_fmaf(squares, scale, __builtin_ldexpf(n.eps, -2 * down));
+                mean = __builtin_fmaf(squares, scale, again ? __builtin_ldexpf(n.eps, -2 * down) : n.eps);
+                if (again || !__any(!(mean >= SMALL && mean <= LARGE))) break;
+                // (lanes of heads that need none have down = 0, and get the same again)
+                if (!(mean >= SMALL && mean <= LARGE)) {
+                    float top = 0.0f;
+#pragma unroll
+                    for (int p = 0; p < PPL; ++p)
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) top = fmaxf(top, fmaxf(fabsf(f[p][0][e]), fabsf(f[p][1][e])));
+                    const int e0 = exponent(head_max(top, log)), e1 = n.eps > 0.0f ? exponent(n.eps) / 2 : -127;
+                    down = e0 > e1 ? e0 : e1;
+#pragma unroll
+                    for (int p = 0; p < PPL; ++p)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int e = 0; e < VE; ++e) f[p][i][e] = __builtin_ldexpf(f[p][i][e], -down);
+                }
             }
             const float r = __builtin_amdgcn_rsqf(mean);             // (within one unit in the last place)
             if constexpr (BACK) dot = dot * r * scale;
@@ -228,7 +232,8 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
                         if constexpr (!BACK) f[p][i][e] = norm * w[p][i][e];
                         else {
                             const float part = d[p][i][e] * norm;
-                            sum[side][p][i][e] += there ? part : 0.0f;
+                            sum[0][p][i][e] += there && !side ? part : 0.0f;
+                            sum[1][p][i][e] += there && side ? part : 0.0f;
                             f[p][i][e] = r * __builtin_fmaf(-norm, dot, w[p][i][e] * d[p][i][e]);
                             if (down != 0) f[p][i][e] = __builtin_ldexpf(f[p][i][e], -down);
                         }
@@ -246,8 +251,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) {
                 if (base + u >= sh.steps) continue;
-                if (base + u < sh.q_steps) take(u, base + u, std::integral_constant<int, 0>());
-                else take(u, base + u, std::integral_constant<int, 1>());
+                take(u, base + u);
             }
             base += BATCH;
             if (base < sh.steps) fetch(base);
@@ -331,7 +335,7 @@ template <bool BACK> hipError_t launch(const NormJob& n, hipStream_t st)
     const int tokens = (64 >> sh.lanes_log) >> sh.heads_log;
     sh.stretches = (j.tokens + tokens - 1) / tokens;
     // backward as many workgroups as are at work at once: eight values a vector take registers for two a compute unit, fewer for three and more (19 200 tokens,
-    // 40 heads of 128 in bfloat16: 125 us with 2, 160 with 3, 134 with 4); forward a wavefront for every stretch (129 us, 136 - 143 with fewer)
+    // 40 heads of 128 in bfloat16: 120 us with 2, 153 with 3); forward a wavefront for every stretch (129 us, 136 - 143 with fewer)
     const long groups = (sh.stretches + WAVES - 1) / WAVES, at_once = (ve == 8 ? 2L : 3L) * units, most = BACK ? (at_once < NORM_GROUPS ? at_once : NORM_GROUPS) : 1L << 22;
     const dim3 grid((unsigned)(groups < most ? groups : most)), block(THREADS);
     size_t lds = (size_t)WAVES * tokens * j.pairs * sizeof(float2);
