@@ -2,7 +2,7 @@
 //
 // For each sequence and key head: s_j = scale q.k_j for the query heads that read the key head, the softmax over the
 // cached tokens j, and the weighted sum of the v_j.  Keys and values are read once, so memory bounds it: 4 * dim * heads operations for
-// 2 * dim * heads / group values (200 003 tokens of 8 key heads, 128 values in bfloat16: 131 us, 6.3 TB/s, where plain reads reach 7.2; 6.6 over
+// 2 * dim * heads / group values (200 003 tokens of 8 key heads, 128 values in bfloat16: 129 us, 6.4 TB/s, where plain reads reach 7.2; 6.6 over
 // 32 x 8 192 tokens).  A cache in 8 bits has half the bytes (200 003 tokens: 80 us, of which 64 are at 6.5 TB/s and the rest the way to the first tile and the join).  More than 16 query heads a key head are blocks of 16, and every block reads the keys and values again.
 // One pass: every wavefront takes tiles of consecutive tokens and keeps, for up to 16 query heads, the running maximum m, the sum l of e^(s - m) and the sum o of e^(s - m) v (times a power of two, see Tiles::bits); a tile with a larger maximum scales l and o by e^(m - m').
 // Parts of a sequence (wavefronts of a workgroup, then workgroups) are joined the same way.
