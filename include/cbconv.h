@@ -527,7 +527,7 @@ int cb_cache_bound(const cb_cache *cache, const int32_t *since_dev, void *hip_st
  * scores, ties to the lowest, `budget` in all or as many as there are.  chosen_dev (n_seq x n_kv_heads x budget) receives the pages' places in the
  * sequence's table, ascending, -1 behind them; count_dev (n_seq x n_kv_heads) how many.  Scores grow with the scale of an attention where that is positive. */
 typedef struct {
-    int32_t budget;            /* >= 1 */
+    int32_t budget;            /* 1 .. 2^30 */
     int32_t first, recent;     /* >= 0, together no more than budget */
     int32_t reserved;          /* must be zero */
 } cb_choose_params;
@@ -536,7 +536,7 @@ int cb_cache_choose(const cb_cache *cache, const cb_choose_params *params, const
 
 /* cb_cache_attend over the tokens of chosen pages alone: those that row (s, key head) of chosen_dev (rows of `budget`) names, count_dev of
  * them.  Counts are taken as 0 .. the sequence's pages or budget, whichever is less; places outside 0 .. max_pages - 1 and pages behind the last token hold
- * no token; a page that is named twice counts twice.  accumulate is refused. */
+ * no token; a page that is named twice counts twice.  budget 1 .. 2^30; accumulate is refused. */
 int cb_cache_attend_chosen(const cb_cache *cache, const cb_attend_params *params, const cb_heads *q, const cb_heads *out,
                            float *lse_dev, const int32_t *chosen_dev, const int32_t *count_dev, int32_t budget,
                            void *hip_stream);

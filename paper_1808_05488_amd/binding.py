@@ -1056,8 +1056,8 @@ class TokenCache:
         i = self._index
         dtype, address = self._values(q, "q")
         a = _heads(q, "q", dtype, i, self.head_dim, None, self.n_seq)
-        if not 1 <= budget < 2 ** 31:
-            raise AssertionError(f"budget: {budget}; needed: 1 or more")
+        if not 1 <= budget <= 2 ** 30:
+            raise AssertionError(f"budget: {budget}; needed: 1 .. 2^30")
         chosen = torch.empty((self.n_seq, self.n_kv_heads, budget), dtype=torch.int32, device=self.device)
         count = torch.empty((self.n_seq, self.n_kv_heads), dtype=torch.int32, device=self.device)
         status = lib().cb_cache_choose(address, _pack_choose(budget, first, recent, 0), a, chosen.data_ptr(), count.data_ptr(), _raw_stream(i))

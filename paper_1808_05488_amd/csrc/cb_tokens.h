@@ -96,6 +96,7 @@ bool attend_fits(const Cache& c, int q_heads);      // its work can be counted i
 hipError_t launch_attend(const AttendJob& j, const Cache& c, hipStream_t st);
 
 // Bounds of the pages from `since` on (null: of all), and the choice of pages by them.
+constexpr int MOST_CHOSEN = 1 << 30;               // pages of a list
 struct ChooseJob {
     Heads q;
     int budget, first, recent;

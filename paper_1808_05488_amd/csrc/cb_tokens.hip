@@ -338,7 +338,7 @@ int cb_cache_attend_chosen(const cb_cache* cache, const cb_attend_params* params
     cb::Cache c = {};
     cb::AttendJob j = {};
     CB_CHECKED(cb::check_attend(cache, params, q, out, &c, &j));
-    if (params->accumulate || !chosen_dev || !count_dev || budget < 1) return CB_EINVAL;
+    if (params->accumulate || !chosen_dev || !count_dev || budget < 1 || budget > cb::MOST_CHOSEN) return CB_EINVAL;
     CB_CHECKED(cb::check_cache(cache, true, q->heads, &c));
     if (!cb::attend_fits(c, q->heads)) return CB_EINVAL;
     j.lse = lse_dev;
@@ -362,7 +362,7 @@ int cb_cache_choose(const cb_cache* cache, const cb_choose_params* params, const
                     void* hip_stream)
 {
     if (!params || !q || params->reserved != 0 || !chosen_dev || !count_dev) return CB_EINVAL;
-    if (params->budget < 1 || params->first < 0 || params->recent < 0 || (long)params->first + params->recent > params->budget) return CB_EINVAL;
+    if (params->budget < 1 || params->budget > cb::MOST_CHOSEN || params->first < 0 || params->recent < 0 || (long)params->first + params->recent > params->budget) return CB_EINVAL;
     cb::Cache c = {};
     CB_CHECKED(cb::check_cache(cache, true, 0, &c));
     cb::ChooseJob j = {};

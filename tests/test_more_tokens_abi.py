@@ -86,7 +86,7 @@ def test_bound_and_choose_refusals():
     def call(c=bytes_cache(), budget=4, first=1, recent=2, reserved=0, q=heads(8), chosen=FAKE, count=FAKE):
         return L.cb_cache_choose(ref(c), C.byref(binding.cb_choose_params(budget, first, recent, reserved)), ref(q), chosen, count, None)
 
-    for kw in (dict(c=None), dict(c=cache()), dict(budget=0), dict(budget=-4), dict(first=-1), dict(recent=-1), dict(first=2, recent=3),
+    for kw in (dict(c=None), dict(c=cache()), dict(budget=0), dict(budget=-4), dict(budget=2 ** 30 + 1), dict(budget=2 ** 31 - 1), dict(first=-1), dict(recent=-1), dict(first=2, recent=3),
                dict(first=2 ** 31 - 1, recent=2 ** 31 - 1, budget=2 ** 31 - 1), dict(reserved=1), dict(q=None), dict(q=heads(6)), dict(q=heads(8, data=None)),
                dict(q=heads(8, data=FAKE + 1)), dict(chosen=None), dict(count=None)):
         assert call(**kw) == EINVAL, kw
@@ -98,6 +98,9 @@ def test_bound_and_choose_refusals():
         assert L.cb_cache_scratch_bytes(C.byref(c), 0, C.byref(n)) == OK
         sizes.append(n.value)
     assert sizes[1] >= 2 * 4 * (1 << 12) * 4 > sizes[0]
+    # pages of all sequences and heads are counted in 32 bits
+    for f in (lambda c: L.cb_cache_bound(C.byref(c), None, None), lambda c: call(c=c)):
+        assert f(bytes_cache(n_seq=1024, n_kv_heads=64, max_pages=1 << 14, weight_dev=None, scratch_bytes=1 << 62)) == EINVAL
     assert call(c=cache(weight_dev=None, max_pages=1 << 12, bounds_dev=11 * FAKE, scratch_bytes=sizes[0])) == ENOMEM
 
 
@@ -109,7 +112,7 @@ def test_attend_chosen_refusals():
         return L.cb_cache_attend_chosen(ref(c), C.byref(p), ref(q), ref(out), None, chosen, count, budget, None)
 
     for kw in (dict(c=None), dict(q=None), dict(out=None), dict(q=heads(6), out=heads(6)), dict(out=heads(4)), dict(scale=math.inf), dict(cap=-1.0),
-               dict(decay=2.0), dict(accumulate=1), dict(chosen=None), dict(count=None), dict(budget=0), dict(budget=-1), dict(q=heads(8, data=None))):
+               dict(decay=2.0), dict(accumulate=1), dict(chosen=None), dict(count=None), dict(budget=0), dict(budget=-1), dict(budget=2 ** 30 + 1), dict(q=heads(8, data=None))):
         assert call(**kw) == EINVAL, kw
     assert call(c=bytes_cache(scratch_bytes=100)) == ENOMEM
 
