@@ -441,11 +441,11 @@ hipError_t launch_bound(const int32_t* since, const Cache& c, hipStream_t st)
 {
     const long most = (long)c.seqs * c.heads * c.max_pages, want = 8L * device_units();
     const dim3 grid((unsigned)(most < want ? most : want)), block(BOUND_THREADS);
-    const int bytes = c.dim * (c.e4m3 ? 1 : (c.bf16 ? 2 : 4)) / 64;      // of a row, for each of 64 lanes
+    // (a row has 64 lanes at most: 4 bytes each where those reach)
 #define CB_BOUND(type, b) hipLaunchKernelGGL((bound_kernel<type, b>), grid, block, 0, st, since, c)
     if (c.e4m3) CB_BOUND(uint8_t, 4);
     else if (c.bf16) {
-        if (bytes <= 4) CB_BOUND(uint16_t, 4);
+        if (c.dim <= 128) CB_BOUND(uint16_t, 4);
         else CB_BOUND(uint16_t, 8);
     } else {
         if (c.dim <= 64) CB_BOUND(float, 4);

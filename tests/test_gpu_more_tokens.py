@@ -732,7 +732,8 @@ KINDS = ["f32", "bf16", "e4m3", "odd"]
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("heads,dim,page", [(2, 64, 16), (3, 80, 32), (1, 256, 64), (8, 128, 128), (2, 16, 1024), (2, 8, 16), (1, 248, 32), (3, 72, 16)])
+@pytest.mark.parametrize("heads,dim,page", [(2, 64, 16), (3, 80, 32), (1, 256, 64), (8, 128, 128), (2, 16, 1024), (2, 8, 16), (1, 248, 32), (3, 72, 16),
+                                            (2, 136, 32), (1, 144, 64), (2, 152, 16), (1, 160, 16), (1, 120, 32)])
 def test_bounds(kind, heads, dim, page):
     if dim % 16 and kind in ("e4m3", "odd"):
         pytest.skip("heads of 8 bits are multiples of 16")
@@ -800,7 +801,8 @@ def check_choose(c, q, lengths, budget, first, recent):
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("heads,group,dim,page,budget,first,recent", [(2, 1, 64, 16, 8, 1, 2), (1, 4, 128, 64, 3, 0, 0), (3, 5, 80, 16, 33, 2, 4), (2, 17, 16, 32, 4, 2, 2),
                                                                       (1, 2, 256, 16, 1, 0, 0), (4, 3, 48, 16, 1000, 1, 1), (2, 2, 8, 16, 5, 0, 1),
-                                                                      (1, 6, 248, 32, 7, 1, 0), (2, 9, 72, 16, 12, 0, 3)])
+                                                                      (1, 6, 248, 32, 7, 1, 0), (2, 9, 72, 16, 12, 0, 3), (2, 2, 136, 16, 5, 0, 1),
+                                                                      (1, 3, 152, 32, 4, 1, 1)])
 def test_choose(kind, heads, group, dim, page, budget, first, recent):
     if dim % 16 and kind in ("e4m3", "odd"):
         pytest.skip("heads of 8 bits are multiples of 16")
@@ -990,6 +992,30 @@ def test_what_choosing_refuses():
                  lambda: c.choose(q[:, :3].contiguous(), 3)):
         with pytest.raises(RuntimeError):
             call()
+
+
+# ---------------------------------------------------------------- all head sizes
+@pytest.mark.parametrize("dim", range(8, 257, 8))
+def test_norm_of_every_head_size(dim):
+    for i, pairs in enumerate([(dim // 2,), (dim // 2 - 1,), (dim // 4, 1), (dim // 8, 0, dim // 8)]):
+        for dtype, layout in ((F32, cb.CB_PAIRS_ADJACENT), (BF16, cb.CB_PAIRS_HALVES)):
+            test_norm_rotate_and_its_gradients(dtype, (F32, BF16)[i % 2], layout, cb.CB_LADDER_SHARED, dim, pairs, 1 + i, 3, 9)
+
+
+@pytest.mark.parametrize("dim", range(16, 257, 16))
+def test_append_in_8_bits_of_every_head_size(dim):
+    for pairs in ((dim // 2,), (dim // 2 - 1,), (dim // 4, 1, 1)):
+        for dtype, layout in ((F32, cb.CB_PAIRS_ADJACENT), (BF16, cb.CB_PAIRS_HALVES)):
+            test_append_in_8_bits_with_rotation(dtype, layout, dim, pairs)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dim", range(8, 257, 8))
+def test_pages_of_every_head_size(kind, dim):
+    if dim % 16 and kind in ("e4m3", "odd"):
+        pytest.skip("heads of 8 bits are multiples of 16")
+    test_bounds(kind, 2, dim, 32)
+    test_attend_over_chosen_pages(kind, 2, 3, dim, 16, 5, 1, 1)
 
 
 # ---------------------------------------------------------------- together
