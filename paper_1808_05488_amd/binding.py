@@ -796,7 +796,8 @@ class Rotary:
                     k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
         """Every head of q over the root of its mean square (and eps), times q_weight (head_dim values, float32 or bfloat16), turned by positions as by
         rotate; k with it by k_weight: q_out, or (q_out, k_out).  q, k and the weights may be parts of a graph (once: gradients of gradients are
-        refused), if their outputs are not given.  An output may be its input."""
+        refused), if their outputs are not given.  An output may be its input.  (A backward pass is recorded into a HIP graph as torch asks for it:
+        while none made outside of the capture, of the same leaves, is alive.)"""
         if (k is None) != (k_weight is None):
             raise AssertionError("k and k_weight are given together")
         if torch.is_grad_enabled() and (q.requires_grad or q_weight.requires_grad or (k is not None and (k.requires_grad or k_weight.requires_grad))):

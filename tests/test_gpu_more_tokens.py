@@ -1,5 +1,6 @@
 """Norms of heads with their rotation and gradients, caches in 8 bits, bounds of pages and attention over those that are chosen, on the GPU against plain
 implementations in 64 bits on the host; a run of them together; streams, graphs and what Python refuses."""
+import ctypes as C
 import math
 import types
 
@@ -304,6 +305,65 @@ def test_norm_on_another_stream_and_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(again, step()):
             assert torch.equal(a, b), i
+
+
+def test_a_training_step_of_norms_in_a_graph():
+    """forward, backward() and a step of the weights in one graph, with eager work on leaves of its own between the replays."""
+    rng = np.random.default_rng(11)
+    n, dim, pairs = 130, 48, (8, 4, 12)
+    x, g = dev(rng.standard_normal((n, 3, dim)), BF16), dev(rng.standard_normal((n, 3, dim)), BF16)
+    w = dev(1 + 0.1 * rng.standard_normal(dim), F32)
+    pos, rot = dev(rng.integers(0, 99, (n, 3)).astype(np.int32)), cb.Rotary(dim, pairs)
+
+    def step(q, w):
+        q.grad = w.grad = None
+        rot.norm_rotate(q, pos, w).backward(g)
+        with torch.no_grad():
+            w -= 0.01 * w.grad
+        return q.grad, w.grad
+
+    held, eager = ([t.clone().requires_grad_() for t in (x, w)] for _ in range(2))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*held)
+    torch.cuda.current_stream().wait_stream(side)
+    with torch.no_grad():
+        held[1].copy_(w)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        grads = step(*held)
+    for i in range(4):
+        with torch.no_grad():
+            x.copy_(dev(rng.standard_normal(x.shape), BF16))
+            held[0].copy_(x)
+            eager[0].copy_(x)
+        graph.replay()
+        again = [t.clone() for t in grads] + [held[1].detach().clone()]
+        torch.cuda.synchronize()
+        for a, b in zip(again, step(*eager) + (eager[1],)):
+            assert torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim,pairs", [(64, (8, 12, 12)), (72, (7, 9, 9)), (256, (31,))])
+def test_gradients_in_the_place_of_what_they_come_from(dtype, dim, pairs):
+    """cb_norm_rotate_back where x_grad is out_grad."""
+    rng = np.random.default_rng([dim, 12])
+    n, heads = 90, 5
+    q, w, g = dev(rng.standard_normal((n, heads, dim)), dtype).requires_grad_(), dev(rng.standard_normal(dim), F32).requires_grad_(), dev(rng.standard_normal((n, heads, dim)), dtype)
+    pos, rot = dev(rng.integers(0, 99, (n, len(pairs))).astype(np.int32)), cb.Rotary(dim, pairs)
+    want = torch.autograd.grad(rot.norm_rotate(q, pos, w, eps=1e-5), (q, w), g)
+    L = cb.binding.lib()
+    at = lambda t: cb.binding.cb_heads(t.data_ptr(), heads * dim, dim, heads, 0)      # noqa: E731
+    gw, size = torch.empty_like(w), C.c_size_t()
+    assert L.cb_norm_rotate_back_scratch_bytes(C.byref(rot.plan), C.byref(size)) == 0
+    scratch = torch.empty(size.value, dtype=torch.uint8, device="cuda")
+    back = cb.binding.cb_norm_back(at(q), at(g), at(g), w.data_ptr(), gw.data_ptr())
+    assert L.cb_norm_rotate_back(C.byref(rot.plan), 1 if dtype == BF16 else 0, n, pos.data_ptr(), 1e-5, 0, C.byref(back), None, scratch.data_ptr(), size.value,
+                                 torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(g, want[0]) and torch.equal(gw, want[1])
 
 
 def test_what_norm_rotate_refuses():
@@ -992,6 +1052,20 @@ def test_what_choosing_refuses():
                  lambda: c.choose(q[:, :3].contiguous(), 3)):
         with pytest.raises(RuntimeError):
             call()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("seqs", [64, 65, 300])
+def test_attend_over_pages_of_many_sequences(kind, seqs):
+    rng = np.random.default_rng([seqs, 83])
+    lengths = [int(x) for x in rng.integers(0, 200, seqs)]
+    lengths[seqs // 2], lengths[-1] = 1500, 0
+    c = with_bounds(rng, kind, lengths, 2, 32, 16)
+    c.bound()
+    q = dev(rng.standard_normal((seqs, 6, 32)), F32 if kind in ("f32", "odd") else BF16)
+    check_chosen(c, q, lengths, check_choose(c, q, lengths, 6, 1, 1))
+    if kind in ("e4m3", "odd"):
+        check_attend_bytes(c, q, lengths)
 
 
 # ---------------------------------------------------------------- all head sizes
