@@ -713,6 +713,25 @@ class _Rotation(torch.autograd.Function):
         return None, None, None, back[0], back[1]
 
 
+# A leaf's gradient is added up on the stream that was current when the first graph of the leaf was made, as long as one is alive.  A backward pass that is
+# recorded into a HIP graph would have that stream wait for the recording one, which ends the process: so graphs leave their stream with their leaves.
+_LEAF = type(torch.autograd.graph.get_gradient_edge(torch.empty(0, requires_grad=True)).node)
+_MADE_ON = "stream of the first norm_rotate"
+
+
+def _mark_leaves(out: torch.Tensor) -> None:
+    for node, _ in out.grad_fn.next_functions:
+        if type(node) is _LEAF:
+            node.metadata.setdefault(_MADE_ON, _raw_stream(out.get_device()))
+
+
+def _check_leaves(nodes, need, index: int) -> None:
+    here = _raw_stream(index)
+    for (node, _), wanted in zip(nodes, need):
+        if wanted and type(node) is _LEAF and node.metadata.get(_MADE_ON, here) != here:
+            raise AssertionError("a backward pass is recorded into a HIP graph while a graph of the same leaves, made on another stream, is alive: drop that one first")
+
+
 class _NormRotation(torch.autograd.Function):
     """Rotary.norm_rotate in a graph."""
 
@@ -730,6 +749,8 @@ class _NormRotation(torch.autograd.Function):
     def _gradients(ctx, q_grad, k_grad):
         positions, q, q_weight, k, k_weight = ctx.saved_tensors
         need = ctx.needs_input_grad
+        if torch.cuda.is_current_stream_capturing():
+            _check_leaves(ctx.next_functions, need[2:], q.get_device())
         return (None, None, None) + ctx.rotary._norm_back(positions, ctx.eps, (q, q_weight, q_grad, need[3], need[4]), (k, k_weight, k_grad, need[5], need[6]))
 
     # (what refuses gradients of gradients takes 4 us of the host's time: only where there may be some)
@@ -796,14 +817,15 @@ class Rotary:
                     k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
         """Every head of q over the root of its mean square (and eps), times q_weight (head_dim values, float32 or bfloat16), turned by positions as by
         rotate; k with it by k_weight: q_out, or (q_out, k_out).  q, k and the weights may be parts of a graph (once: gradients of gradients are
-        refused), if their outputs are not given.  An output may be its input.  (A backward pass is recorded into a HIP graph as torch asks for it:
-        while none made outside of the capture, of the same leaves, is alive.)"""
+        refused), if their outputs are not given.  An output may be its input.  A backward pass that is recorded into a HIP graph is
+        refused while a graph of the same leaves, made on another stream, is alive."""
         if (k is None) != (k_weight is None):
             raise AssertionError("k and k_weight are given together")
         if torch.is_grad_enabled() and (q.requires_grad or q_weight.requires_grad or (k is not None and (k.requires_grad or k_weight.requires_grad))):
             if q_out is not None or k_out is not None:
                 raise AssertionError("outputs that are given carry no gradient: norm_rotate without them, or under torch.no_grad()")
             q_out, k_out = _NormRotation.apply(self, eps, positions, q, q_weight, k, k_weight)
+            _mark_leaves(q_out if q_out.requires_grad else k_out)
             return q_out if k is None else (q_out, k_out)
         if k is None and k_out is not None:
             raise AssertionError("k_out without k")

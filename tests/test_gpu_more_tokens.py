@@ -1,6 +1,7 @@
 """Norms of heads with their rotation and gradients, caches in 8 bits, bounds of pages and attention over those that are chosen, on the GPU against plain
 implementations in 64 bits on the host; a run of them together; streams, graphs and what Python refuses."""
 import ctypes as C
+import gc
 import math
 import types
 
@@ -344,6 +345,36 @@ def test_a_training_step_of_norms_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(again, step(*eager) + (eager[1],)):
             assert torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("leaf", ["q", "weight", "k"])
+def test_a_recorded_backward_pass_is_refused_while_another_graph_of_the_leaves_lives(leaf):
+    rng = np.random.default_rng(13)
+    x, w = dev(rng.standard_normal((20, 2, 16)), BF16), dev(rng.standard_normal(16), F32)
+    t = (w if leaf == "weight" else x).clone().requires_grad_()
+    pos, rot, g = torch.zeros((20, 1), dtype=torch.int32, device="cuda"), cb.Rotary(16, (8,)), torch.ones_like(x)
+
+    def step():
+        if leaf == "k":
+            return rot.norm_rotate(x, pos, w, k=t, k_weight=w)[1]
+        return rot.norm_rotate(x, pos, t) if leaf == "weight" else rot.norm_rotate(t, pos, w)
+
+    alive = step()
+    want = torch.autograd.grad(alive, t, g, retain_graph=True)[0]
+    torch.cuda.synchronize()
+    with pytest.raises(AssertionError, match="same leaves"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            torch.autograd.grad(step(), t, g)
+    del alive
+    gc.collect()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = torch.autograd.grad(step(), t, g)[0]
+    for _ in range(3):
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
