@@ -382,7 +382,7 @@ int cb_select_thresholds(const cb_stage *stages, int32_t n_stages, const void *c
  * keep nothing themselves: every one is described by its arguments, enqueued on hip_stream, asynchronous, and free
  * of allocations, memsets and host decisions that depend on device data, so it may be captured into a HIP graph.
  * Values are float32 or bfloat16, a cache may hold them in 8 bits; everything between them is computed in float32 or more.  Calls that
- * share a cache or a scratch buffer run on one stream, or are ordered by the caller. */
+ * share a cache or a scratch buffer run on one stream, or are ordered by the caller.  Arrays and hip_stream are of the current device. */
 
 /* A tensor of heads: value i of head h of token n is data_dev[n * token_stride + h * head_stride + i] (strides in values;
  * any sign and order, the values of a head are contiguous).  heads * head_dim values a token. */

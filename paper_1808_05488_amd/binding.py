@@ -659,6 +659,8 @@ assert 3 * struct.calcsize("@Pqqii") + 2 * struct.calcsize("@P") == C.sizeof(cb_
 _NO_HEADS = _pack_heads(0, 0, 0, 0, 0)
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
+# (Kernels go to the current device, whose default stream has the same address as every other's: calls on tensors of another one make that one current first.)
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
 def _heads(t: torch.Tensor, what: str, dtype, index: int, dim: int, heads: Optional[int] = None, tokens: Optional[int] = None) -> bytes:
@@ -794,6 +796,9 @@ class Rotary:
         n, dtype, index, dim = q.shape[0], q.dtype, q.get_device(), self.head_dim
         if index < 0 or dtype not in _CB_DT:
             raise AssertionError(f"q: {dtype} on {q.device}; needed: float32 or bfloat16 on a GPU")
+        if index != _current_device():
+            with torch.cuda.device(index):
+                return self.rotate(q, positions, k, inverse, q_out, k_out)
         a, c, d = _heads(q, "q", dtype, index, dim), None, None
         if q_out is None:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
@@ -832,6 +837,9 @@ class Rotary:
         n, dtype, index, dim, wdtype = q.shape[0], q.dtype, q.get_device(), self.head_dim, q_weight.dtype
         if index < 0 or dtype not in _CB_DT or wdtype not in _CB_DT:
             raise AssertionError(f"q: {dtype} on {q.device}, q_weight: {wdtype}; needed: float32 or bfloat16 on a GPU")
+        if index != _current_device():
+            with torch.cuda.device(index):
+                return self.norm_rotate(q, positions, q_weight, k, k_weight, eps, q_out, k_out)
         a, c, d, w = _heads(q, "q", dtype, index, dim), None, None, None
         if q_out is None:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
@@ -1000,6 +1008,9 @@ class TokenCache:
         if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad):
             _refuse_grad("append")
         n, i, dim = k.shape[0], self._index, self.head_dim
+        if i != _current_device():
+            with torch.cuda.device(i):
+                return self.append(k, v, positions, rotary, q, offsets, start, q_out)
         dtype, address = self._values(k, "k")
         a = _heads(k, "k", dtype, i, dim, self.n_kv_heads)
         b = _heads(v, "v", dtype, i, dim, self.n_kv_heads, n)
@@ -1030,6 +1041,9 @@ class TokenCache:
         if q.requires_grad:
             _refuse_grad("attend")
         i, dim = self._index, self.head_dim
+        if i != _current_device():
+            with torch.cuda.device(i):
+                return self.attend(q, scale, softcap, accumulate, decay, out, lse, chosen)
         dtype, address = self._values(q, "q")
         a = _heads(q, "q", dtype, i, dim, None, self.n_seq)
         heads = q.shape[1]
@@ -1067,6 +1081,9 @@ class TokenCache:
         """Bring the bounds up to date, of the pages with slots from since[s] (int32; not given: 0) to the last token of sequence s: after an append
         from what it started at, after an eviction all."""
         i = self._index
+        if i != _current_device():
+            with torch.cuda.device(i):
+                return self.bound(since)
         status = lib().cb_cache_bound(self._address, _dense(since, "since", torch.int32, i, (self.n_seq,)), _raw_stream(i))
         if status:
             _check(status, "cb_cache_bound")
@@ -1077,6 +1094,9 @@ class TokenCache:
         if q.requires_grad:
             _refuse_grad("choose")
         i = self._index
+        if i != _current_device():
+            with torch.cuda.device(i):
+                return self.choose(q, budget, first, recent)
         dtype, address = self._values(q, "q")
         a = _heads(q, "q", dtype, i, self.head_dim, None, self.n_seq)
         if not 1 <= budget <= 2 ** 30:
@@ -1093,6 +1113,9 @@ class TokenCache:
         """Cut every sequence back to `budget` tokens a key head: those of the newest `window` steps of time, then those with the
         most weight.  weight, time, lengths: what to go by instead of the cache's own, which receive what is left."""
         i = self._index
+        if i != _current_device():
+            with torch.cuda.device(i):
+                return self.evict(budget, window, weight, time, lengths)
         status = lib().cb_cache_evict(self._address, _pack_evict(
             budget, window, _dense(weight, "weight", torch.float32, i, self._slots) or 0,
             _dense(time, "time", torch.int32, i, self._slots) or 0, _dense(lengths, "lengths", torch.int32, i, (self.n_seq,)) or 0),

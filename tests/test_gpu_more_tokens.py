@@ -1197,6 +1197,48 @@ def test_bounds_after_an_eviction(kind):
     check_chosen(c, q, lengths, check_choose(c, q, lengths, 2, 0, 1))
 
 
+def test_calls_on_another_device_than_the_current_one(monkeypatch):
+    """Such calls make the tensors' device current for themselves.  (Which one is current is made up here: there may be one alone.)"""
+    rng = np.random.default_rng(94)
+    made, at = [], [0]
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            made.append(self.index)
+            at.append(self.index)
+
+        def __exit__(self, *_):
+            at.pop()
+
+    dim, rot = 16, cb.Rotary(16, (8,))
+    x, w, pos, g = dev(rng.standard_normal((2, 2, dim)), BF16), dev(rng.standard_normal(dim), F32), dev(np.array([[3], [4]], np.int32)), torch.ones((2, 2, dim), dtype=BF16, device="cuda")
+    leaf = x.clone().requires_grad_()
+
+    def work():
+        c = cb.TokenCache.create(2, 2, dim, 64, dtype=BF16, page_tokens=16, bounded=True)
+        y = rot.norm_rotate(x, pos, w)
+        grad, = torch.autograd.grad(rot.norm_rotate(leaf, pos, w), leaf, g)
+        q = c.append(rot.rotate(x, pos), x, pos, rot, q=y)
+        c.bound()
+        pick = c.choose(q, 1)
+        out = c.attend(q, chosen=pick) + c.attend(q, accumulate=True)
+        c.evict(1)
+        return (y, grad, q, c.k_pages, c.bounds, c.weight) + pick + out
+
+    want = work()
+    assert not made
+    monkeypatch.setattr(cb.binding, "_current_device", lambda: at[-1])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    at[0] = 1
+    got = work()
+    assert made == [0] * 9 and at == [1]
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
 def test_two_streams_at_once():
     """Caches and plans of their own on streams of their own: results are those of one after the other."""
     rng = np.random.default_rng(93)
