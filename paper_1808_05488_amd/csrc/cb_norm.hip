@@ -72,8 +72,8 @@ template <int VE, bool ADJACENT> __device__ __forceinline__ void turn_by(const f
     }
 }
 
-// PPL: pieces of a head that a lane has (more than one where single values are taken of heads above 128).
-template <typename T, int VE, int PPL, bool ADJACENT, bool BACK>
+// PPL: pieces of a head that a lane has (more than one where single values are taken of heads above 128).  CACHED: loads and stores go through the caches.
+template <typename T, int VE, int PPL, bool ADJACENT, bool CACHED, bool BACK>
 __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Shape sh)
 {
     typedef Vec<T, VE> V;
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
         };
         auto get = [](bool there, const T* from) {
             W v = W{};
-            if (there) v = __builtin_nontemporal_load(reinterpret_cast<const W*>(from));
+            if (there) v = CACHED ? *reinterpret_cast<const W*>(from) : __builtin_nontemporal_load(reinterpret_cast<const W*>(from));
             return v;
         };
         auto fetch = [&](int base) {
@@ -243,8 +243,8 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
                 V y, z;
 #pragma unroll
                 for (int e = 0; e < VE; ++e) { narrow(f[p][0][e], y.e[e]); narrow(f[p][1][e], z.e[e]); }
-                if (has_a[p]) store_once<false>(y, dst + first[p]);
-                if (has_b[p]) store_once<false>(z, dst + second[p]);
+                if (has_a[p]) store_once<CACHED>(y, dst + first[p]);
+                if (has_b[p]) store_once<CACHED>(z, dst + second[p]);
             }
         };
         for (int base = 0; base < sh.steps;) {
@@ -340,17 +340,25 @@ template <bool BACK> hipError_t launch(const NormJob& n, hipStream_t st)
     const dim3 grid((unsigned)(groups < most ? groups : most)), block(THREADS);
     size_t lds = (size_t)WAVES * tokens * j.pairs * sizeof(float2);
     if (BACK && lds < WAVES * 2 * j.dim * sizeof(float)) lds = WAVES * 2 * j.dim * sizeof(float);
-#define CB_NORM(type, v, p, adjacent) hipLaunchKernelGGL((norm_kernel<type, v, p, adjacent, BACK>), grid, block, lds, st, n, sh)
-#define CB_NORMS(type, v) do { if (j.adjacent) CB_NORM(type, v, 1, true); else CB_NORM(type, v, 1, false); } while (0)
+    // Around the caches where a load or store of a wavefront has whole lines, or nearly so: first and second values of pairs apart, each of 128, 192 or more
+    // bytes.  Where two of them share the lines, the caches bring these together.  (19 200 tokens, 40 heads in bfloat16, around and through the caches: halves of
+    // 128 values 68 and 76 us, 64: 46 and 43, 96: 73 and 62, adjacent pairs of 128: 112 and 78, gradients 146 and 131; 9 600 tokens in float32, halves of 64: 36 and
+    // 42, 80: 57 and 54, 96: 60 and 62, adjacent pairs of 128: 131 and 84.)
+    const int half = j.pairs * (j.bf16 ? 2 : 4);
+    const bool around = !j.adjacent && 2 * j.pairs == j.dim && ve * (j.bf16 ? 2 : 4) == 16 && (half == 128 || half >= 192);
+#define CB_NORM(type, v, p, adjacent, cached) hipLaunchKernelGGL((norm_kernel<type, v, p, adjacent, cached, BACK>), grid, block, lds, st, n, sh)
+#define CB_NORMS(type, v) do { if (j.adjacent) CB_NORM(type, v, 1, true, true); else CB_NORM(type, v, 1, false, true); } while (0)
     if (j.bf16) {
-        if (ve == 8) CB_NORMS(uint16_t, 8);
+        if (around) CB_NORM(uint16_t, 8, 1, false, false);
+        else if (ve == 8) CB_NORMS(uint16_t, 8);
         else if (ve == 4) CB_NORMS(uint16_t, 4);
         else if (ve == 2) CB_NORMS(uint16_t, 2);
-        else CB_NORM(uint16_t, 1, 2, false);
+        else CB_NORM(uint16_t, 1, 2, false, true);
     } else {
-        if (ve == 4) CB_NORMS(float, 4);
+        if (around) CB_NORM(float, 4, 1, false, false);
+        else if (ve == 4) CB_NORMS(float, 4);
         else if (ve == 2) CB_NORMS(float, 2);
-        else CB_NORM(float, 1, 2, false);
+        else CB_NORM(float, 1, 2, false, true);
     }
 #undef CB_NORMS
 #undef CB_NORM
