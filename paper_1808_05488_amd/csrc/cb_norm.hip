@@ -5,13 +5,14 @@
 // heads of g n.  Since mean(w g n) = r mean(w g x), both sums over a head are made in one go.
 //
 // Heads are independent and read once, so memory bounds it: 2 values' bytes forward, 3 backward.  38 400 tokens x 40 heads of 128 in bfloat16 take 130 us (6.0
-// TB/s, reads and writes; a copy around the caches reaches 6.4), the gradients of 19 200 such tokens 120 us (4.9 TB/s: two wavefronts a SIMD with all that they hold, and
-// no more registers for a third) and 5 for the sums of the weights'.  A head lies in the registers of 1 - 64 lanes (two
+// TB/s, reads and writes; a copy around the caches reaches 6.4), the gradients of 19 200 such tokens 113 us (5.2 TB/s, three wavefronts a SIMD: what
+// they hold takes all registers for them) and 5 for the sums of the weights'.  A head lies in the registers of 1 - 64 lanes (two
 // vectors of 16 bytes a lane, as pairs need them), its sums take a few steps across them.  A wavefront goes through all heads of its tokens by itself: the
 // angles, which it makes once, and all that addresses need stay in its registers.  (With a workgroup for a token, its angles in LDS and a division for every head the
 // clip took 208 us.)
-// A gradient of the weights is summed in registers by persistent workgroups, each of which leaves one row of sums; a second launch adds these
-// up in order, so that results do not vary.  (The next heads' loads before this one's arithmetic: 13 us more.  Queries and keys, and heads that are
+// A gradient of the weights is summed by persistent workgroups, the queries' in registers, the keys', which are fewer, in LDS; each leaves one row of sums, and a
+// second launch adds these up in order, so that results do not vary.  (Both in registers, and the angles too, left room for two wavefronts a SIMD: 125 us in all instead of 118,
+// heads of 80 values 116 instead of 96; but of 256 values 219 instead of 226.)  (The next heads' loads before this one's arithmetic: 13 us more.  Queries and keys, and heads that are
 // scaled, in code of their own, 24 KB instead of 16: 6 us more.)
 #include <climits>
 #include <type_traits>
@@ -74,13 +75,13 @@ template <int VE, bool ADJACENT> __device__ __forceinline__ void turn_by(const f
 
 // PPL: pieces of a head that a lane has (more than one where single values are taken of heads above 128).  CACHED: loads and stores go through the caches.
 template <typename T, int VE, int PPL, bool ADJACENT, bool CACHED, bool BACK>
-__global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Shape sh)
+__global__ __launch_bounds__(THREADS, BACK && VE == 8 ? 3 : 1) void norm_kernel(const NormJob n, const Shape sh)
 {
     typedef Vec<T, VE> V;
     typedef typename Word<sizeof(V)>::type W;
     constexpr int BATCH = BACK ? 2 : 3;          // steps that are on their way at once
     extern __shared__ __align__(16) float2 s_dyn[];      // a wavefront's angles; BACK: its sums in the end
-    __shared__ __align__(16) float s_w[2][MAX_DIM];
+    __shared__ __align__(16) float s_w[2][MAX_DIM + 8];       // behind the weights what there is for no value: zero
     const RotaryJob& j = n.r;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), np = j.pairs, dim = j.dim;
     const int log = sh.lanes_log, sub = lane & ((1 << log) - 1), slot = lane >> log, head0 = slot & ((1 << sh.heads_log) - 1), token = slot >> sh.heads_log;
@@ -92,6 +93,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
         const int d = i < dim ? i : i - dim;
         s_w[i < dim ? 0 : 1][d] = from ? weight_of(from, n.weight_bf16, d) : 0.0f;
     }
+    if (tid < 16) s_w[tid / 8][MAX_DIM + tid % 8] = 0.0f;
     __syncthreads();
     // where a lane's pieces lie in a head, the same of every head
     int first[PPL], second[PPL];
@@ -104,16 +106,25 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
         second[p] = turns[p] && !j.adjacent ? np + VE * piece : 2 * VE * piece + VE;
         has_a[p] = piece < sh.pieces;
         has_b[p] = has_a[p] && second[p] < dim;
+        if (!has_a[p]) first[p] = MAX_DIM;
+        if (!has_b[p]) second[p] = MAX_DIM;
     }
-    float sum[2][PPL][2][VE] = {};               // BACK: of g n, of all heads that were here
+    // BACK: of g n, of all heads that were here (the keys' in LDS, where a lane has a place of its own)
+    constexpr int VALUES = PPL * 2 * VE;
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    __shared__ __align__(16) f32x4 s_keys[BACK ? VALUES / 4 : 1][BACK ? THREADS : 1];
+    float sum[VALUES] = {};
+    if constexpr (BACK)
+#pragma unroll
+        for (int i = 0; i < VALUES / 4; ++i) s_keys[i][tid] = f32x4{0, 0, 0, 0};
 
     for (long stretch = (long)blockIdx.x * WAVES + wave; stretch < sh.stretches; stretch += (long)gridDim.x * WAVES) {
-        const long tok = stretch * tokens + token;
+        const uint32_t tok = (uint32_t)(stretch * tokens) + (uint32_t)token;      // (there are less than 2^31)
         const bool real = tok < j.tokens;
         W x[BATCH][PPL][2], g[BATCH][PPL][2];
         // (by value: a choice between the arguments' addresses would put them all into scratch memory)
         auto head_at = [&](bool q, Heads a, Heads b, int h) {
-            return (const T*)(q ? a.data : b.data) + tok * (q ? a.token : b.token) + (long)h * (q ? a.head : b.head);
+            return (const T*)(q ? a.data : b.data) + (long)tok * (q ? a.token : b.token) + (long)h * (q ? a.head : b.head);
         };
         auto get = [](bool there, const T* from) {
             W v = W{};
@@ -141,9 +152,14 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
             }
         };
         fetch(0);
-        float2 at[PPL][VE];
+        auto angles = [&](int p, float2 (&to)[VE]) {
+#pragma unroll
+            for (int e = 0; e < VE; ++e) to[e] = turns[p] ? s_cs[token * np + (sub + (p << log)) * VE + e] : make_float2(1.0f, 0.0f);
+        };
+        float2 at[PPL][VE];                      // (forward: backward there are no registers for them)
         {
             // (the last stretch's angles have been read: a wavefront's accesses of LDS are in order)
+            __builtin_amdgcn_wave_barrier();
             for (int i = lane; i < tokens * np; i += 64) {
                 const int t = i / np;
                 const long y = stretch * tokens + t;
@@ -152,11 +168,10 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            if constexpr (!BACK) {
 #pragma unroll
-            for (int p = 0; p < PPL; ++p)
-#pragma unroll
-                for (int e = 0; e < VE; ++e) at[p][e] = turns[p] ? s_cs[token * np + (sub + (p << log)) * VE + e] : make_float2(1.0f, 0.0f);
-            __builtin_amdgcn_wave_barrier();
+                for (int p = 0; p < PPL; ++p) angles(p, at[p]);
+            }
         }
         auto take = [&](int u, int step) {
             const bool side = step >= sh.q_steps;                    // keys
@@ -170,8 +185,8 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
                 if constexpr (BACK) { ga = __builtin_bit_cast(V, g[u][p][0]); gb = __builtin_bit_cast(V, g[u][p][1]); }
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
-                    w[p][0][e] = has_a[p] ? s_w[side][first[p] + e] : 0.0f;
-                    w[p][1][e] = has_b[p] ? s_w[side][second[p] + e] : 0.0f;
+                    w[p][0][e] = s_w[side][first[p] + e];
+                    w[p][1][e] = s_w[side][second[p] + e];
                     f[p][0][e] = widen(xa.e[e]);
                     f[p][1][e] = widen(xb.e[e]);
                     if constexpr (BACK) {
@@ -179,7 +194,10 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
                         d[p][1][e] = widen(gb.e[e]);
                     }
                 }
-                if constexpr (BACK) turn_by<VE, ADJACENT>(at[p], d[p][0], d[p][1]);
+                if constexpr (BACK) {
+                    angles(p, at[p]);
+                    turn_by<VE, ADJACENT>(at[p], d[p][0], d[p][1]);
+                }
             }
             float mean, dot;
             int down = 0;                                            // f is the head times 2^-down
@@ -218,10 +236,27 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
                             for (int e = 0; e < VE; ++e) f[p][i][e] = __builtin_ldexpf(f[p][i][e], -down);
                 }
             }
-            const float r = __builtin_amdgcn_rsqf(mean);             // (within one unit in the last place)
+            // (within one unit in the last place; of a head that is not there all is zero then)
+            const float r = there ? __builtin_amdgcn_rsqf(mean) : 0.0f;
             if constexpr (BACK) dot = dot * r * scale;
             T* dst = (T*)head_at(!side, j.q_out, j.k_out, h);
             const bool stored = (side ? j.k_out.data : j.q_out.data) != nullptr;
+            if constexpr (BACK) {
+                auto add = [&](int v, float to) {
+                    const int p = v / (2 * VE), i = v / VE % 2, e = v % VE;
+                    return __builtin_fmaf(d[p][i][e], f[p][i][e] * r, to);
+                };
+                if (!side) {
+#pragma unroll
+                    for (int v = 0; v < VALUES; ++v) sum[v] = add(v, sum[v]);
+                } else {
+#pragma unroll
+                    for (int v = 0; v < VALUES; v += 4) {
+                        const f32x4 to = s_keys[v / 4][tid];
+                        s_keys[v / 4][tid] = f32x4{add(v, to[0]), add(v + 1, to[1]), add(v + 2, to[2]), add(v + 3, to[3])};
+                    }
+                }
+            }
 #pragma unroll
             for (int p = 0; p < PPL; ++p) {
 #pragma unroll
@@ -231,9 +266,6 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
                         const float norm = f[p][i][e] * r;
                         if constexpr (!BACK) f[p][i][e] = norm * w[p][i][e];
                         else {
-                            const float part = d[p][i][e] * norm;
-                            sum[0][p][i][e] += there && !side ? part : 0.0f;
-                            sum[1][p][i][e] += there && side ? part : 0.0f;
                             f[p][i][e] = r * __builtin_fmaf(-norm, dot, w[p][i][e] * d[p][i][e]);
                             if (down != 0) f[p][i][e] = __builtin_ldexpf(f[p][i][e], -down);
                         }
@@ -270,7 +302,8 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormJob n, const Sh
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int e = 0; e < VE; ++e) {
-                        float v = sum[side][p][i][e];
+                        const int at = (p * 2 + i) * VE + e;
+                        float v = side ? s_keys[at / 4][tid][at % 4] : sum[at];
                         for (int k = log; k < 6; ++k) v += __shfl_xor(v, 1 << k);
                         const int d = (i ? second[p] : first[p]) + e;
                         const bool has = i ? has_b[p] : has_a[p];
@@ -334,9 +367,9 @@ template <bool BACK> hipError_t launch(const NormJob& n, hipStream_t st)
     }
     const int tokens = (64 >> sh.lanes_log) >> sh.heads_log;
     sh.stretches = (j.tokens + tokens - 1) / tokens;
-    // backward as many workgroups as are at work at once: eight values a vector take registers for two a compute unit, fewer for three and more (19 200 tokens,
-    // 40 heads of 128 in bfloat16: 120 us with 2, 153 with 3); forward a wavefront for every stretch (129 us, 136 - 143 with fewer)
-    const long groups = (sh.stretches + WAVES - 1) / WAVES, at_once = (ve == 8 ? 2L : 3L) * units, most = BACK ? (at_once < NORM_GROUPS ? at_once : NORM_GROUPS) : 1L << 22;
+    // backward as many workgroups as are at work at once, three a compute unit (19 200 tokens, 40 heads of 128 in bfloat16: 118 us, 129 with two); forward a
+    // wavefront for every stretch (129 us, 136 - 143 with fewer)
+    const long groups = (sh.stretches + WAVES - 1) / WAVES, at_once = 3L * units, most = BACK ? (at_once < NORM_GROUPS ? at_once : NORM_GROUPS) : 1L << 22;
     const dim3 grid((unsigned)(groups < most ? groups : most)), block(THREADS);
     size_t lds = (size_t)WAVES * tokens * j.pairs * sizeof(float2);
     if (BACK && lds < WAVES * 2 * j.dim * sizeof(float)) lds = WAVES * 2 * j.dim * sizeof(float);
