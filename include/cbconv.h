@@ -428,13 +428,13 @@ int cb_rotate(const cb_rotary *rotary, int32_t dtype, int64_t n_tokens, const in
 
 /* Norm and rotate: n = x / sqrt(mean(x^2) + eps) for every head x of q (and k), times q_weight_dev (k_weight_dev; head_dim values of weight_dtype, CB_F32
  * or CB_BF16), then rotated as by cb_rotate and rounded once.  eps >= 0, finite (0: a head of zeros is not a number afterwards).  Mean squares outside
- * 2^-100 .. 2^100 are computed in float64.  k, k_weight_dev and k_out are NULL together.  An output may be its own input, with its strides. */
+ * 2^-100 .. 2^100 are made of the head times a power of two, so that none overflows or vanishes.  k, k_weight_dev and k_out are NULL together.  An output may be its own input, with its strides. */
 int cb_norm_rotate(const cb_rotary *rotary, int32_t dtype, int64_t n_tokens, const int32_t *positions_dev, float eps,
                    int32_t weight_dtype, const cb_heads *q, const void *q_weight_dev, const cb_heads *q_out,
                    const cb_heads *k, const void *k_weight_dev, const cb_heads *k_out, void *hip_stream);
 /* Its gradients, of q, of k or of both (NULL: not this one): x and weight_dev as they went in, out_grad the gradient of what came out; x_grad
  * (data_dev NULL: not wanted) and weight_grad_dev (NULL: not wanted) receive those of x and of the weight.  Weights' gradients are summed over all tokens and heads in
- * a fixed order (that depends on sizes, on which of q and k there are and on the GPU's compute units alone) and rounded once; with any of them scratch_dev has
+ * a fixed order (that depends on sizes, strides, alignment, which of q and k there are and the GPU's compute units alone) and rounded once; with any of them scratch_dev has
  * cb_norm_rotate_back_scratch_bytes, 16-byte aligned.  x_grad may be out_grad, with its strides, and overlaps no other tensor. */
 typedef struct {
     cb_heads x, out_grad, x_grad;

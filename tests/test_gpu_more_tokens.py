@@ -1099,6 +1099,36 @@ def test_attend_over_pages_of_many_sequences(kind, seqs):
         check_attend_bytes(c, q, lengths)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("off", [0, 1, 3])
+def test_queries_and_answers_of_any_strides(kind, off):
+    """Rows of a wider tensor, heads apart, from addresses that divide into no vector; what lies between stays as it was."""
+    rng = np.random.default_rng([off, 84])
+    lengths, heads, hq, dim = [700, 0, 33, 2000], 2, 6, 80
+    dtype = F32 if kind in ("f32", "odd") else BF16
+    c = with_bounds(rng, kind, lengths, heads, dim, 16)
+    c.bound()
+    pitch, step = (hq + 1) * (dim + off) + off, dim + off
+    flat, room = dev(rng.standard_normal(4 * pitch + 8), dtype), torch.full((4 * pitch + 8,), 7.0, dtype=dtype, device="cuda")
+    view = lambda t: t.as_strided((4, hq, dim), (pitch, step, 1), off + step)      # noqa: E731
+    q, out = view(flat), view(room)
+    plain = q.contiguous()
+    pick, same = c.choose(q, 5, first=1, recent=1), c.choose(plain, 5, first=1, recent=1)
+    assert torch.equal(pick[0], same[0]) and torch.equal(pick[1], same[1])
+    for kw in ({}, {"chosen": pick}):
+        want = c.attend(plain, **kw)
+        room.fill_(7.0)
+        got = c.attend(q, out=out, **kw)
+        assert got[0].data_ptr() == out.data_ptr() and torch.equal(out, want[0]) and torch.equal(got[1], want[1])
+        kept = room.clone()
+        view(kept).fill_(7.0)
+        assert (kept == 7.0).all()
+        # one query head's tensor, the same for all sequences
+        shared = plain[:1, :1].expand(4, 2, dim)
+        a, b = c.attend(shared, **kw), c.attend(shared.contiguous(), **kw)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 # ---------------------------------------------------------------- all head sizes
 @pytest.mark.parametrize("dim", range(8, 257, 8))
 def test_norm_of_every_head_size(dim):
