@@ -717,20 +717,24 @@ class _Rotation(torch.autograd.Function):
 
 # A leaf's gradient is added up on the stream that was current when the first graph of the leaf was made, as long as one is alive.  A backward pass that is
 # recorded into a HIP graph would have that stream wait for the recording one, which ends the process: so graphs leave their stream with their leaves.
-_LEAF = type(torch.autograd.graph.get_gradient_edge(torch.empty(0, requires_grad=True)).node)
 _MADE_ON = "stream of the first norm_rotate"
+
+
+def _is_leaf(node) -> bool:
+    # (by name: the type is not to be had without a tensor that wants a gradient, which an import in inference mode cannot make)
+    return type(node).__name__ == "AccumulateGrad"
 
 
 def _mark_leaves(out: torch.Tensor) -> None:
     for node, _ in out.grad_fn.next_functions:
-        if type(node) is _LEAF:
+        if _is_leaf(node):
             node.metadata.setdefault(_MADE_ON, _raw_stream(out.get_device()))
 
 
 def _check_leaves(nodes, need, index: int) -> None:
     here = _raw_stream(index)
     for (node, _), wanted in zip(nodes, need):
-        if wanted and type(node) is _LEAF and node.metadata.get(_MADE_ON, here) != here:
+        if wanted and _is_leaf(node) and node.metadata.get(_MADE_ON, here) != here:
             raise AssertionError("a backward pass is recorded into a HIP graph while a graph of the same leaves, made on another stream, is alive: drop that one first")
 
 
