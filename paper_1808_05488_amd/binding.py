@@ -689,6 +689,16 @@ def _dense(t: Optional[torch.Tensor], what: str, dtype, index: int, shape) -> Op
     return t.data_ptr()
 
 
+def _given(*outs) -> tuple:
+    """Those outputs that are given."""
+    return tuple(t for t in outs if t is not None)
+
+
+# Kernels write through addresses, past torch, whose graphs go by a tensor's version to find that what they have saved is still there: outputs that were
+# given, which may be an input that a graph has saved, get a new one.  (0.7 us, for calls that give some.)
+_written = torch.autograd.graph.increment_version
+
+
 def _refuse_grad(where: str) -> None:
     if torch.is_grad_enabled():
         raise AssertionError(f"{where} carries no gradient: give it detached tensors, or call it under torch.no_grad()")
@@ -789,7 +799,7 @@ class Rotary:
                q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
         """q (tokens x heads x head_dim) turned by positions (tokens x axes, int32), and k with it: q_out, or (q_out, k_out).
         inverse: turned back, which is also the gradient of q from that of q_out: q and k may be parts of a graph, if their outputs are not
-        given.  An output may be its input."""
+        given.  An output may be its input, and is changed for torch's graphs too: one that has saved it finds out in its backward pass."""
         if (q.requires_grad or (k is not None and k.requires_grad)) and torch.is_grad_enabled():
             if q_out is not None or k_out is not None:
                 raise AssertionError("outputs that are given carry no gradient: rotate without them, or under torch.no_grad()")
@@ -797,6 +807,7 @@ class Rotary:
             return q_out if k is None else (q_out, k_out)
         if k is None and k_out is not None:
             raise AssertionError("k_out without k")
+        given = () if q_out is None and k_out is None else _given(q_out, k_out)
         n, dtype, index, dim = q.shape[0], q.dtype, q.get_device(), self.head_dim
         if index < 0 or dtype not in _CB_DT:
             raise AssertionError(f"q: {dtype} on {q.device}; needed: float32 or bfloat16 on a GPU")
@@ -820,13 +831,15 @@ class Rotary:
                                  a, b, c, d, 1 if inverse else 0, _raw_stream(index))
         if status:
             _check(status, "cb_rotate")
+        if given:
+            _written(given)
         return q_out if k is None else (q_out, k_out)
 
     def norm_rotate(self, q: torch.Tensor, positions: torch.Tensor, q_weight: torch.Tensor, k: Optional[torch.Tensor] = None,
                     k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
         """Every head of q over the root of its mean square (and eps), times q_weight (head_dim values, float32 or bfloat16), turned by positions as by
         rotate; k with it by k_weight: q_out, or (q_out, k_out).  q, k and the weights may be parts of a graph (once: gradients of gradients are
-        refused), if their outputs are not given.  An output may be its input.  A backward pass that is recorded into a HIP graph is
+        refused), if their outputs are not given.  An output may be its input, as with rotate.  A backward pass that is recorded into a HIP graph is
         refused while a graph of the same leaves, made on another stream, is alive."""
         if (k is None) != (k_weight is None):
             raise AssertionError("k and k_weight are given together")
@@ -838,6 +851,7 @@ class Rotary:
             return q_out if k is None else (q_out, k_out)
         if k is None and k_out is not None:
             raise AssertionError("k_out without k")
+        given = () if q_out is None and k_out is None else _given(q_out, k_out)
         n, dtype, index, dim, wdtype = q.shape[0], q.dtype, q.get_device(), self.head_dim, q_weight.dtype
         if index < 0 or dtype not in _CB_DT or wdtype not in _CB_DT:
             raise AssertionError(f"q: {dtype} on {q.device}, q_weight: {wdtype}; needed: float32 or bfloat16 on a GPU")
@@ -861,6 +875,8 @@ class Rotary:
                                       a, _dense(q_weight, "q_weight", wdtype, index, (dim,)), b, c, w, d, _raw_stream(index))
         if status:
             _check(status, "cb_norm_rotate")
+        if given:
+            _written(given)
         return q_out if k is None else (q_out, k_out)
 
     def _norm_back(self, positions, eps, *sides):
@@ -903,7 +919,8 @@ class TokenCache:
     heads x 2 x head_dim, of the pages' type, with 8 bits bfloat16): needed to choose pages.  scratch, if
     it is given (caches may share one): dense uint8, 256-byte aligned, scratch_bytes(query heads) long, and zeroed before the first call.  Calls run on
     the current stream; calls that share a cache or a scratch buffer have to be on one stream, or ordered.  A graph that
-    has recorded calls needs the object as long as it is replayed: its scratch buffers stay until then."""
+    has recorded calls needs the object as long as it is replayed: its scratch buffers stay until then.  Calls write the cache's own tensors past torch's
+    autograd, which does not notice: what has saved them for a backward pass (other code's attention over the pages, say) has to be through with it before."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
                  weight: Optional[torch.Tensor] = None, time: Optional[torch.Tensor] = None,
@@ -1011,6 +1028,7 @@ class TokenCache:
         sequence's are not written).  Tensors that want a gradient are refused."""
         if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad):
             _refuse_grad("append")
+        given = () if q_out is None else _given(q_out)
         n, i, dim = k.shape[0], self._index, self.head_dim
         if i != _current_device():
             with torch.cuda.device(i):
@@ -1035,6 +1053,8 @@ class TokenCache:
             a, b, c, d, _raw_stream(i))
         if status:
             _check(status, "cb_cache_append")
+        if given:
+            _written(given)
         return q_out
 
     def attend(self, q: torch.Tensor, scale: Optional[float] = None, softcap: float = 0.0, accumulate: bool = False,
@@ -1044,6 +1064,7 @@ class TokenCache:
         those pages alone (and not to accumulate).  A q that wants a gradient is refused."""
         if q.requires_grad:
             _refuse_grad("attend")
+        given = () if out is None and lse is None else _given(out, lse)
         i, dim = self._index, self.head_dim
         if i != _current_device():
             with torch.cuda.device(i):
@@ -1079,6 +1100,8 @@ class TokenCache:
             status = lib().cb_cache_attend_chosen(address, params, a, b, lse.data_ptr(), pages_at, count_at, pages.shape[2], _raw_stream(i))
         if status:
             _check(status, "cb_cache_attend" if chosen is None else "cb_cache_attend_chosen")
+        if given:
+            _written(given)
         return out, lse
 
     def bound(self, since: Optional[torch.Tensor] = None) -> None:
