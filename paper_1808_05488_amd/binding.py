@@ -690,8 +690,11 @@ def _dense(t: Optional[torch.Tensor], what: str, dtype, index: int, shape) -> Op
 
 
 def _given(*outs) -> tuple:
-    """Those outputs that are given."""
-    return tuple(t for t in outs if t is not None)
+    """Those outputs that are given.  One that wants a gradient is refused where it would be part of a graph: what is written to it carries none."""
+    given = tuple(t for t in outs if t is not None)
+    if torch.is_grad_enabled() and any(t.requires_grad for t in given):
+        raise AssertionError("an output that is given carries no gradient: give a detached one, or call under torch.no_grad()")
+    return given
 
 
 # Kernels write through addresses, past torch, whose graphs go by a tensor's version to find that what they have saved is still there: outputs that were

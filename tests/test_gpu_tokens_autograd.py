@@ -46,6 +46,18 @@ def test_a_graph_notices_that_what_it_has_saved_was_written(which):
 
 
 @pytest.mark.parametrize("which", GIVEN)
+def test_outputs_that_want_a_gradient(which):
+    t = output(which, requires_grad=True)
+    before = t.detach().clone()
+    with pytest.raises(AssertionError, match="carries no gradient"):
+        GIVEN[which](values(), t)
+    assert torch.equal(t, before)
+    with torch.no_grad():
+        GIVEN[which](values(), t)
+    assert not torch.equal(t, before)
+
+
+@pytest.mark.parametrize("which", GIVEN)
 def test_outputs_in_inference_mode(which):
     t = output(which)
     before = t.clone()
