@@ -702,6 +702,16 @@ def _given(*outs) -> tuple:
 _written = torch.autograd.graph.increment_version
 
 
+# Forward-mode derivatives live beside tensors at a level that is entered (torch.autograd.forward_ad.dual_level), and kernels see the values alone.
+_dual = torch.autograd.forward_ad
+_in_dual_level = (lambda: _dual._current_level >= 0) if hasattr(_dual, "_current_level") else (lambda: True)
+
+
+def _refuse_tangents(*tensors) -> None:
+    if any(t is not None and _dual.unpack_dual(t).tangent is not None for t in tensors):
+        raise AssertionError("token operators carry no forward-mode derivatives: give them tensors without a tangent")
+
+
 def _refuse_grad(where: str) -> None:
     if torch.is_grad_enabled():
         raise AssertionError(f"{where} carries no gradient: give it detached tensors, or call it under torch.no_grad()")
@@ -802,7 +812,8 @@ class Rotary:
                q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
         """q (tokens x heads x head_dim) turned by positions (tokens x axes, int32), and k with it: q_out, or (q_out, k_out).
         inverse: turned back, which is also the gradient of q from that of q_out: q and k may be parts of a graph, if their outputs are not
-        given.  An output may be its input, and is changed for torch's graphs too: one that has saved it finds out in its backward pass."""
+        given.  An output may be its input, and is changed for torch's graphs too: one that has saved it finds out in its backward pass.  Forward-mode
+        derivatives are refused."""
         if (q.requires_grad or (k is not None and k.requires_grad)) and torch.is_grad_enabled():
             if q_out is not None or k_out is not None:
                 raise AssertionError("outputs that are given carry no gradient: rotate without them, or under torch.no_grad()")
@@ -810,6 +821,8 @@ class Rotary:
             return q_out if k is None else (q_out, k_out)
         if k is None and k_out is not None:
             raise AssertionError("k_out without k")
+        if _in_dual_level():
+            _refuse_tangents(q, k, q_out, k_out)
         given = () if q_out is None and k_out is None else _given(q_out, k_out)
         n, dtype, index, dim = q.shape[0], q.dtype, q.get_device(), self.head_dim
         if index < 0 or dtype not in _CB_DT:
@@ -854,6 +867,8 @@ class Rotary:
             return q_out if k is None else (q_out, k_out)
         if k is None and k_out is not None:
             raise AssertionError("k_out without k")
+        if _in_dual_level():
+            _refuse_tangents(q, q_weight, k, k_weight, q_out, k_out)
         given = () if q_out is None and k_out is None else _given(q_out, k_out)
         n, dtype, index, dim, wdtype = q.shape[0], q.dtype, q.get_device(), self.head_dim, q_weight.dtype
         if index < 0 or dtype not in _CB_DT or wdtype not in _CB_DT:
@@ -1031,6 +1046,8 @@ class TokenCache:
         sequence's are not written).  Tensors that want a gradient are refused."""
         if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad):
             _refuse_grad("append")
+        if _in_dual_level():
+            _refuse_tangents(k, v, q, q_out)
         given = () if q_out is None else _given(q_out)
         n, i, dim = k.shape[0], self._index, self.head_dim
         if i != _current_device():
@@ -1067,6 +1084,8 @@ class TokenCache:
         those pages alone (and not to accumulate).  A q that wants a gradient is refused."""
         if q.requires_grad:
             _refuse_grad("attend")
+        if _in_dual_level():
+            _refuse_tangents(q, out, lse)
         given = () if out is None and lse is None else _given(out, lse)
         i, dim = self._index, self.head_dim
         if i != _current_device():
@@ -1123,6 +1142,8 @@ class TokenCache:
         `first` first and the `recent` last ones, then the highest scores; places in the sequence's table, ascending, -1 behind them, and how many."""
         if q.requires_grad:
             _refuse_grad("choose")
+        if _in_dual_level():
+            _refuse_tangents(q)
         i = self._index
         if i != _current_device():
             with torch.cuda.device(i):

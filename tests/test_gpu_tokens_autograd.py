@@ -92,3 +92,20 @@ def test_inputs_and_new_outputs_keep_their_version():
     cache.append(x, x)
     out, lse = cache.attend(x)
     assert [t._version for t in tensors] == before and a._version == b._version == out._version == lse._version == 0
+
+
+def test_forward_mode_and_batched_gradients_are_refused():
+    rot, pos, w, cache = operands()
+    x = values()
+    with torch.autograd.forward_ad.dual_level():
+        d = torch.autograd.forward_ad.make_dual(x, x)
+        for call in (lambda: rot.norm_rotate(d, pos, w), lambda: rot.rotate(d, pos), lambda: cache.append(d, x), lambda: cache.attend(d), lambda: cache.choose(d, 1)):
+            with pytest.raises(AssertionError, match="forward-mode"):
+                call()
+        assert torch.equal(rot.rotate(x, pos), x)
+    with pytest.raises(AssertionError, match="forward-mode"):
+        torch.func.jvp(lambda t: rot.norm_rotate(t, pos, w), (x,), (x,))
+    q = x.clone().requires_grad_()
+    for f in (lambda t: rot.norm_rotate(t, pos, w), lambda t: rot.rotate(t, pos)):
+        with pytest.raises(RuntimeError):
+            torch.autograd.grad(f(q), q, torch.stack([x, x]), is_grads_batched=True)
