@@ -1293,3 +1293,44 @@ def test_two_streams_at_once():
     for i in range(2):
         for g in got[i]:
             assert all(torch.equal(a, b) for a, b in zip(g, want[i]))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("layout", [cb.CB_PAIRS_HALVES, cb.CB_PAIRS_ADJACENT])
+@pytest.mark.parametrize("dim,pairs", [(64, (24,)), (128, (16, 8, 8)), (72, (20,)), (24, (10,)), (40, (15,)), (256, (31,)), (128, (32,))])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_what_is_not_finite_behind_the_pairs_stays_in_its_place(dtype, layout, dim, pairs, bad):
+    """Values behind the pairs are not turned: what one of them is shows nowhere else, but through the mean of its head."""
+    rng = np.random.default_rng([dim, 71])
+    n, heads = 5, 3
+    x, w, g = rng.standard_normal((n, heads, dim)), rng.standard_normal(dim), rng.standard_normal((n, heads, dim))
+    pos, rot = dev(rng.integers(1, 99, (n, len(pairs))).astype(np.int32)), cb.Rotary(dim, pairs, layout=layout)
+
+    def step(x, w, g):
+        a, b = dev(x, dtype).requires_grad_(), dev(w, F32).requires_grad_()
+        y = rot.norm_rotate(a, pos, b)
+        return [t.detach().cpu() for t in (y, *torch.autograd.grad(y, (a, b), dev(g, dtype)))]
+
+    def but(t, *at):
+        t = t.copy()
+        t[at] = bad
+        return t
+
+    clean = step(x, w, g)
+    first = 2 * sum(pairs)
+    for d in sorted({first, first + 1, (first + dim) // 2, dim - 1}):
+        other = torch.arange(dim) != d
+        # of x: 1 / infinity is zero, and so is all of the head but that value; what is not a number is in the whole head
+        y = step(but(x, 1, 2, d), w, g)[0]
+        assert torch.isnan(y[1, 2, d])
+        assert torch.isnan(y[1, 2]).all() if math.isnan(bad) else (y[1, 2, other] == 0).all()
+        kept = torch.ones((n, heads), dtype=torch.bool)
+        kept[1, 2] = False
+        assert torch.equal(y[kept], clean[0][kept])
+        # of the weight: that value of all heads; its own gradient does not hang on it, the others' do by the mean alone
+        y, _, gw = step(x, but(w, d), g)
+        assert not torch.isfinite(y[..., d]).any() and torch.equal(y[..., other], clean[0][..., other]) and torch.equal(gw, clean[2])
+        # of the output's gradient: that weight's gradient, and the head's
+        y, gx, gw = step(x, w, but(g, 1, 2, d))
+        assert torch.equal(y, clean[0]) and torch.equal(gx[kept], clean[1][kept])
+        assert not torch.isfinite(gw[d]) and torch.equal(gw[other], clean[2][other])
