@@ -428,7 +428,7 @@ int cb_rotate(const cb_rotary *rotary, int32_t dtype, int64_t n_tokens, const in
 
 /* Norm and rotate: n = x / sqrt(mean(x^2) + eps) for every head x of q (and k), times q_weight_dev (k_weight_dev; head_dim values of weight_dtype, CB_F32
  * or CB_BF16), then rotated as by cb_rotate and rounded once.  eps >= 0, finite (0: a head of zeros is not a number afterwards).  Mean squares outside
- * 2^-100 .. 2^100 are made of the head times a power of two, so that none overflows or vanishes.  k, k_weight_dev and k_out are NULL together.  An output may be its own input, with its strides. */
+ * 2^-100 .. 2^100 (2^-40 .. 2^40 for gradients) are made of the head times a power of two, so that none overflows or vanishes.  k, k_weight_dev and k_out are NULL together.  An output may be its own input, with its strides. */
 int cb_norm_rotate(const cb_rotary *rotary, int32_t dtype, int64_t n_tokens, const int32_t *positions_dev, float eps,
                    int32_t weight_dtype, const cb_heads *q, const void *q_weight_dev, const cb_heads *q_out,
                    const cb_heads *k, const void *k_weight_dev, const cb_heads *k_out, void *hip_stream);

@@ -24,8 +24,9 @@ namespace cb {
 namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64, MAX_DIM = 256;
-// Mean squares in float32 are exact enough, and their root's inverse is a normal number, between these; what is beyond is scaled by a power of two first.
-constexpr float SMALL = 0x1p-100f, LARGE = 0x1p100f;
+// Mean squares in float32 are exact enough, and their root's inverse is a normal number, between these; what is beyond is scaled by a power of two first.  Backward
+// the sum of x times gradients and weights has to stay within float32's range, too: values within 2^-20 .. 2^24 leave it most of that.
+constexpr float SMALL = 0x1p-100f, LARGE = 0x1p100f, SMALL_BACK = 0x1p-40f, LARGE_BACK = 0x1p40f;
 
 // How a wavefront's lanes are dealt: 2^lanes_log to a head, of 2^heads_log heads at a time, of as many tokens as are left over.
 struct Shape {
@@ -220,9 +221,10 @@ __global__ __launch_bounds__(THREADS, VE == 8 ? (BACK ? 3 : 4) : 1) void norm_ke
                 squares = head_sum(squares, log);
                 if constexpr (BACK) dot = head_sum(dot, log);
                 mean = __builtin_fmaf(squares, scale, again ? __builtin_ldexpf(n.eps, -2 * down) : n.eps);
-                if (again || !__any(!(mean >= SMALL && mean <= LARGE))) break;
+                const bool fits = mean >= (BACK ? SMALL_BACK : SMALL) && mean <= (BACK ? LARGE_BACK : LARGE);
+                if (again || !__any(!fits)) break;
                 // (lanes of heads that need none have down = 0, and get the same again)
-                if (!(mean >= SMALL && mean <= LARGE)) {
+                if (!fits) {
                     float top = 0.0f;
 #pragma unroll
                     for (int p = 0; p < PPL; ++p)

@@ -1334,3 +1334,15 @@ def test_what_is_not_finite_behind_the_pairs_stays_in_its_place(dtype, layout, d
         y, gx, gw = step(x, w, but(g, 1, 2, d))
         assert torch.equal(y, clean[0]) and torch.equal(gx[kept], clean[1][kept])
         assert not torch.isfinite(gw[d]) and torch.equal(gw[other], clean[2][other])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size,grad", [(1e13, 1e26), (1e-13, 1e-26), (1e-14, 1e-29), (1e8, 1e31), (1e-9, 1e-30), (1e14, 1e-12), (1e-14, 1e10), (1e13, 1e30)])
+def test_gradients_of_the_norm_far_from_one(dtype, size, grad):
+    """Values and gradients whose products leave float32's range, where neither they nor the results do."""
+    rng = np.random.default_rng(72)
+    n, dim, pairs = 9, 64, (8, 12, 12)
+    q, g = dev(size * rng.standard_normal((n, 3, dim)), dtype).requires_grad_(), dev(grad * rng.standard_normal((n, 3, dim)), dtype)
+    w, pos, rot = dev(rng.standard_normal(dim), F32).requires_grad_(), rng.integers(0, 99, (n, 3)).astype(np.int32), cb.Rotary(dim, pairs)
+    gx, gw = torch.autograd.grad(rot.norm_rotate(q, dev(pos), w, eps=0.0), (q, w), g)
+    check_back(q, w, g, pos, pairs, 0, 0, 0.0, gx, gw)
