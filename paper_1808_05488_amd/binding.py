@@ -704,7 +704,6 @@ _written = torch.autograd.graph.increment_version
 
 # Forward-mode derivatives live beside tensors at a level that is entered (torch.autograd.forward_ad.dual_level), and kernels see the values alone.
 _dual = torch.autograd.forward_ad
-_in_dual_level = (lambda: _dual._current_level >= 0) if hasattr(_dual, "_current_level") else (lambda: True)
 
 
 def _refuse_tangents(*tensors) -> None:
@@ -821,7 +820,7 @@ class Rotary:
             return q_out if k is None else (q_out, k_out)
         if k is None and k_out is not None:
             raise AssertionError("k_out without k")
-        if _in_dual_level():
+        if _dual._current_level >= 0:
             _refuse_tangents(q, k, q_out, k_out)
         given = () if q_out is None and k_out is None else _given(q_out, k_out)
         n, dtype, index, dim = q.shape[0], q.dtype, q.get_device(), self.head_dim
@@ -867,7 +866,7 @@ class Rotary:
             return q_out if k is None else (q_out, k_out)
         if k is None and k_out is not None:
             raise AssertionError("k_out without k")
-        if _in_dual_level():
+        if _dual._current_level >= 0:
             _refuse_tangents(q, q_weight, k, k_weight, q_out, k_out)
         given = () if q_out is None and k_out is None else _given(q_out, k_out)
         n, dtype, index, dim, wdtype = q.shape[0], q.dtype, q.get_device(), self.head_dim, q_weight.dtype
@@ -1046,7 +1045,7 @@ class TokenCache:
         sequence's are not written).  Tensors that want a gradient are refused."""
         if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad):
             _refuse_grad("append")
-        if _in_dual_level():
+        if _dual._current_level >= 0:
             _refuse_tangents(k, v, q, q_out)
         given = () if q_out is None else _given(q_out)
         n, i, dim = k.shape[0], self._index, self.head_dim
@@ -1084,7 +1083,7 @@ class TokenCache:
         those pages alone (and not to accumulate).  A q that wants a gradient is refused."""
         if q.requires_grad:
             _refuse_grad("attend")
-        if _in_dual_level():
+        if _dual._current_level >= 0:
             _refuse_tangents(q, out, lse)
         given = () if out is None and lse is None else _given(out, lse)
         i, dim = self._index, self.head_dim
@@ -1142,7 +1141,7 @@ class TokenCache:
         `first` first and the `recent` last ones, then the highest scores; places in the sequence's table, ascending, -1 behind them, and how many."""
         if q.requires_grad:
             _refuse_grad("choose")
-        if _in_dual_level():
+        if _dual._current_level >= 0:
             _refuse_tangents(q)
         i = self._index
         if i != _current_device():
