@@ -438,6 +438,37 @@ __global__ __launch_bounds__((Tile<KT, T, DP>::WAVES * 64)) void attend_kernel(c
         }
     };
 
+    // 8 bits: a query's products with codes, which are up to 448 whatever the keys are, are summed before their scale comes in.  Heads of q with values from
+    // 2^64 on come in times 2^-64, so that these sums stay in range, and their scores times 2^64 in the end.  (When q is here, not where it is asked for:
+    // the rows' loads go out first.)
+    bool untamed = false;
+    float lift = 1.0f;
+    auto tame = [&] {
+        u16x2 size = {0, 0};
+#pragma unroll
+        for (int i = 0; i < QSTEPS; ++i)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) size = __builtin_elementwise_max(size, __builtin_bit_cast(u16x2, q[0][i][y] & 0x7FFF7FFFu));
+        // (a question for the lanes, whose answers fold over the four that have a part of a head: two changes of lanes would take as long as a tile's scores)
+        unsigned long long of = __ballot(size[0] >= (127 + 64) << 7 || size[1] >= (127 + 64) << 7);
+        lift = 1.0f;
+        if (of == 0) return;
+        of |= of >> 32;
+        of |= of >> 16;
+        const bool large = of >> l16 & 1;
+        lift = large ? 0x1p64f : 1.0f;
+        const float down = large ? 0x1p-64f : 1.0f;
+#pragma unroll
+        for (int z = 0; z < QTERMS; ++z)
+#pragma unroll
+            for (int i = 0; i < QSTEPS; ++i)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const float a = __uint_as_float(q[z][i][y] << 16) * down, b = __uint_as_float(q[z][i][y] & 0xFFFF0000u) * down;
+                    q[z][i][y] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+                }
+    };
+
     auto put_sums = [&](long at, float M, float L) {
         if (a.j.lse) a.j.lse[at] = L == 0.0f ? -__builtin_inff() : M + logf(L);
         if (a.scores) a.sums[at] = make_float2(M, L == 0.0f ? 0.0f : 1.0f / L);
@@ -482,6 +513,11 @@ __global__ __launch_bounds__((Tile<KT, T, DP>::WAVES * 64)) void attend_kernel(c
     bool fresh = true;                                         // the next tile begins a stretch
     for (;;) {
         f32x4 sc[SUB];
+        if constexpr (BYTE)
+            if (untamed) {
+                untamed = false;
+                tame();
+            }
         if (here) {
             // scores of tokens 16 * s + 4 * quad + r for query head l16
 #pragma unroll
@@ -516,6 +552,7 @@ __global__ __launch_bounds__((Tile<KT, T, DP>::WAVES * 64)) void attend_kernel(c
                 used = 0;
                 pages = look_up(y, ty);
                 load_q(y);
+                untamed = true;
             } else if (++used == 64 / SUB) {
                 used = 0;
                 pages = ahead;
@@ -534,7 +571,7 @@ __global__ __launch_bounds__((Tile<KT, T, DP>::WAVES * 64)) void attend_kernel(c
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     float y = sc[s][r] * a.j.scale;
-                    if constexpr (BYTE) y *= __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(scales_x.x), used_x * SUB + s));
+                    if constexpr (BYTE) y = y * __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(scales_x.x), used_x * SUB + s)) * lift;
                     if (a.j.softcap > 0.0f) y = a.j.softcap * tanhf(y / a.j.softcap);
                     y = 4 * quad + r < w.left[s] ? y : -__builtin_inff();
                     sc[s][r] = y;

@@ -1346,3 +1346,27 @@ def test_gradients_of_the_norm_far_from_one(dtype, size, grad):
     w, pos, rot = dev(rng.standard_normal(dim), F32).requires_grad_(), rng.integers(0, 99, (n, 3)).astype(np.int32), cb.Rotary(dim, pairs)
     gx, gw = torch.autograd.grad(rot.norm_rotate(q, dev(pos), w, eps=0.0), (q, w), g)
     check_back(q, w, g, pos, pairs, 0, 0, 0.0, gx, gw)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("heads,group,dim", [(2, 3, 64), (1, 17, 128), (3, 1, 80), (2, 2, 256)])
+def test_attend_in_8_bits_of_large_queries_over_small_keys(dtype, heads, group, dim):
+    """A query times a key's codes, before their scale, may be more than float32 holds; heads of ordinary size beside it are what they were."""
+    rng = np.random.default_rng([heads, dim, 73])
+    lengths = [300, 40, 1]
+    c = make_bytes(rng, lengths, heads, dim, 32)
+    q = dev(2 * rng.standard_normal((3, heads * group, dim)), dtype)
+    all_pages = (torch.arange(c.table.shape[1], dtype=torch.int32, device="cuda").expand(3, heads, -1).contiguous(),
+                 torch.full((3, heads), c.table.shape[1], dtype=torch.int32, device="cuda"))
+    ordinary = c.attend(q)[0]
+    large = (q * 2.0 ** 118).to(dtype)
+    c.k_scale.mul_(2.0 ** -52)
+    scale = float(np.float32(2.0 ** -66 * dim ** -0.5))
+    for t in (large, torch.where(torch.arange(heads * group, device="cuda")[None, :, None] % 2 == 0, large, q)):
+        assert torch.isfinite(t).all()
+        check_attend_bytes(c, t, lengths, scale=scale)
+        again, lse = c.attend(t, scale=scale, chosen=all_pages)
+        want = attend64(wide(c), t, lengths, scale, 0.0)
+        within(f64(again), want[0], want[3], "out over chosen pages")
+    c.k_scale.mul_(2.0 ** 52)
+    assert torch.equal(c.attend(q)[0], ordinary)
