@@ -716,30 +716,10 @@ def _refuse_grad(where: str) -> None:
         raise AssertionError(f"{where} carries no gradient: give it detached tensors, or call it under torch.no_grad()")
 
 
-class _Rotation(torch.autograd.Function):
-    """Rotary.rotate in a graph: the gradient of a rotation is the rotation back."""
-
-    @staticmethod
-    def forward(ctx, rotary, inverse, positions, q, k):
-        ctx.rotary, ctx.inverse = rotary, inverse
-        ctx.save_for_backward(positions)
-        ctx.set_materialize_grads(False)
-        out = rotary.rotate(q, positions, k, inverse)
-        q_out, k_out = (out, None) if k is None else out
-        ctx.mark_non_differentiable(*(y for x, y in ((q, q_out), (k, k_out)) if x is not None and not x.requires_grad))
-        return q_out, k_out
-
-    @staticmethod
-    def backward(ctx, *grads):
-        positions, = ctx.saved_tensors
-        # (a gradient comes in any strides: a sum's is one value, repeated)
-        back = [None if g is None else ctx.rotary.rotate(g.contiguous(), positions, inverse=not ctx.inverse) for g in grads]
-        return None, None, None, back[0], back[1]
-
-
 # A leaf's gradient is added up on the stream that was current when the first graph of the leaf was made, as long as one is alive.  A backward pass that is
 # recorded into a HIP graph would have that stream wait for the recording one, which ends the process: so graphs leave their stream with their leaves.
-_MADE_ON = "stream of the first norm_rotate"
+# (Those that are made here: torch does not tell the stream of a graph that other operations made first.)
+_MADE_ON = "stream of the first rotation"
 
 
 def _is_leaf(node) -> bool:
@@ -758,6 +738,29 @@ def _check_leaves(nodes, need, index: int) -> None:
     for (node, _), wanted in zip(nodes, need):
         if wanted and _is_leaf(node) and node.metadata.get(_MADE_ON, here) != here:
             raise AssertionError("a backward pass is recorded into a HIP graph while a graph of the same leaves, made on another stream, is alive: drop that one first")
+
+
+class _Rotation(torch.autograd.Function):
+    """Rotary.rotate in a graph: the gradient of a rotation is the rotation back."""
+
+    @staticmethod
+    def forward(ctx, rotary, inverse, positions, q, k):
+        ctx.rotary, ctx.inverse = rotary, inverse
+        ctx.save_for_backward(positions)
+        ctx.set_materialize_grads(False)
+        out = rotary.rotate(q, positions, k, inverse)
+        q_out, k_out = (out, None) if k is None else out
+        ctx.mark_non_differentiable(*(y for x, y in ((q, q_out), (k, k_out)) if x is not None and not x.requires_grad))
+        return q_out, k_out
+
+    @staticmethod
+    def backward(ctx, *grads):
+        positions, = ctx.saved_tensors
+        if torch.cuda.is_current_stream_capturing():
+            _check_leaves(ctx.next_functions, ctx.needs_input_grad[2:], positions.get_device())
+        # (a gradient comes in any strides: a sum's is one value, repeated)
+        back = [None if g is None else ctx.rotary.rotate(g.contiguous(), positions, inverse=not ctx.inverse) for g in grads]
+        return None, None, None, back[0], back[1]
 
 
 class _NormRotation(torch.autograd.Function):
@@ -812,11 +815,13 @@ class Rotary:
         """q (tokens x heads x head_dim) turned by positions (tokens x axes, int32), and k with it: q_out, or (q_out, k_out).
         inverse: turned back, which is also the gradient of q from that of q_out: q and k may be parts of a graph, if their outputs are not
         given.  An output may be its input, and is changed for torch's graphs too: one that has saved it finds out in its backward pass.  Forward-mode
-        derivatives are refused."""
+        derivatives are refused, and so is a backward pass that is recorded into a HIP graph while a graph of the same leaves is alive that a rotate or norm_rotate on another
+        stream made; of graphs that other operations made there the caller has to take care: torch waits for their stream, which ends the process."""
         if (q.requires_grad or (k is not None and k.requires_grad)) and torch.is_grad_enabled():
             if q_out is not None or k_out is not None:
                 raise AssertionError("outputs that are given carry no gradient: rotate without them, or under torch.no_grad()")
             q_out, k_out = _Rotation.apply(self, inverse, positions, q, k)
+            _mark_leaves(q_out if q_out.requires_grad else k_out)
             return q_out if k is None else (q_out, k_out)
         if k is None and k_out is not None:
             raise AssertionError("k_out without k")
@@ -854,8 +859,8 @@ class Rotary:
                     k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
         """Every head of q over the root of its mean square (and eps), times q_weight (head_dim values, float32 or bfloat16), turned by positions as by
         rotate; k with it by k_weight: q_out, or (q_out, k_out).  q, k and the weights may be parts of a graph (once: gradients of gradients are
-        refused), if their outputs are not given.  An output may be its input, as with rotate.  A backward pass that is recorded into a HIP graph is
-        refused while a graph of the same leaves, made on another stream, is alive."""
+        refused), if their outputs are not given.  An output may be its input, and what is refused in recorded backward
+        passes and forward mode is so, as with rotate."""
         if (k is None) != (k_weight is None):
             raise AssertionError("k and k_weight are given together")
         if torch.is_grad_enabled() and (q.requires_grad or q_weight.requires_grad or (k is not None and (k.requires_grad or k_weight.requires_grad))):

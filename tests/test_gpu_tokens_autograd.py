@@ -1,4 +1,6 @@
 """How the token operators stand to torch's autograd: outputs that are given, modes that carry derivatives."""
+import gc
+
 import pytest
 import torch
 
@@ -109,3 +111,33 @@ def test_forward_mode_and_batched_gradients_are_refused():
     for f in (lambda t: rot.norm_rotate(t, pos, w), lambda t: rot.rotate(t, pos)):
         with pytest.raises(RuntimeError):
             torch.autograd.grad(f(q), q, torch.stack([x, x]), is_grads_batched=True)
+
+
+@pytest.mark.parametrize("first", ["rotate", "norm_rotate"])
+@pytest.mark.parametrize("recorded", ["rotate", "norm_rotate"])
+@pytest.mark.parametrize("as_k", [False, True])
+def test_a_recorded_backward_pass_of_a_leaf_that_another_stream_has_in_a_graph(first, recorded, as_k):
+    rot, pos, w, _ = operands()
+    x, t, g = values(), values().requires_grad_(), values()
+
+    def step(which):
+        if which == "rotate":
+            return rot.rotate(x, pos, k=t)[1] if as_k else rot.rotate(t, pos)
+        return rot.norm_rotate(x, pos, w, k=t, k_weight=w)[1] if as_k else rot.norm_rotate(t, pos, w)
+
+    alive = step(first)
+    want, = torch.autograd.grad(step(recorded), t, g)
+    torch.cuda.synchronize()
+    with pytest.raises(AssertionError, match="same leaves"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            torch.autograd.grad(step(recorded), t, g)
+    del alive
+    gc.collect()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got, = torch.autograd.grad(step(recorded), t, g)
+    for _ in range(3):
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
