@@ -1370,3 +1370,87 @@ def test_attend_in_8_bits_of_large_queries_over_small_keys(dtype, heads, group, 
         within(f64(again), want[0], want[3], "out over chosen pages")
     c.k_scale.mul_(2.0 ** 52)
     assert torch.equal(c.attend(q)[0], ordinary)
+
+
+# ---------------------------------------------------------------- calls with more work than there are wavefronts
+def units():
+    return torch.cuda.get_device_properties(0).multi_processor_count
+
+
+def dealt(dim, pairs, hq, hk, vector):
+    """How a wavefront of the norms is dealt (cb_norm.hip, launch): tokens of a stretch, steps of the queries, of the keys."""
+    pieces = -(-dim // (2 * vector))
+    lanes = 1
+    while lanes < pieces and lanes < 64:
+        lanes *= 2
+    # heads at a time: the fewest lanes without one, the most heads of those that leave as few
+    cost, at_once = min((-(-hq // h) * h + -(-hk // h) * h, -h) for h in (1 << i for i in range(7)) if lanes * h <= 64)
+    return 64 // lanes // -at_once, -(-hq // -at_once), -(-hk // -at_once)
+
+
+@pytest.mark.parametrize("dtype,layout,dim,pairs,hq,hk,vector,n", [(BF16, cb.CB_PAIRS_HALVES, 128, (16, 24, 24), 8, 8, 8, 7001), (F32, cb.CB_PAIRS_ADJACENT, 16, (4, 4), 3, 1, 4, 250003),
+                                                                   (BF16, cb.CB_PAIRS_ADJACENT, 80, (8, 12, 10), 6, 2, 2, 9001), (F32, cb.CB_PAIRS_HALVES, 40, (15,), 5, 2, 1, 13001)])
+def test_gradients_of_more_stretches_than_wavefronts(dtype, layout, dim, pairs, hq, hk, vector, n):
+    """Every wavefront of the backward pass goes through several stretches of tokens, some through one less than others."""
+    rng = np.random.default_rng([dim, n])
+    tokens, q_steps, k_steps = dealt(dim, pairs, hq, hk, vector)
+    waves = 3 * units() * 4
+    stretches = -(-n // tokens)
+    assert stretches > 2 * waves and stretches % waves
+    q, k = dev(rng.standard_normal((n, hq, dim), dtype=np.float32), dtype).requires_grad_(), dev(rng.standard_normal((n, hk, dim), dtype=np.float32), dtype).requires_grad_()
+    gq, gk = dev(rng.standard_normal((n, hq, dim), dtype=np.float32), dtype), dev(rng.standard_normal((n, hk, dim), dtype=np.float32), dtype)
+    wq, wk = (dev(1 + 0.3 * rng.standard_normal(dim), F32).requires_grad_() for _ in range(2))
+    pos, rot, eps = rng.integers(-5, 2000, (n, len(pairs))).astype(np.int32), cb.Rotary(dim, pairs, layout=layout), 1e-3
+    out = rot.norm_rotate(q, dev(pos), wq, k=k, k_weight=wk, eps=eps)
+    got = torch.autograd.grad(out, (q, wq, k, wk), (gq, gk))
+    for x, w, g, y, gx, gw, steps in ((q, wq, gq, out[0], got[0], got[1], q_steps), (k, wk, gk, out[1], got[2], got[3], k_steps)):
+        total, size = np.zeros(dim), np.zeros(dim)
+        for a in range(0, n, 20000):
+            part = slice(a, min(a + 20000, n))
+            check_norm(rot, x[part], w, pos[part], pairs, layout, 0, eps, y[part], "output")
+            check_back(x[part], w, g[part], pos[part], pairs, layout, 0, eps, gx[part], None)
+            _, some, norms, _ = norm_back64(f64(x[part]), f64(w), f64(g[part]), pos[part], pairs, layout, 0, eps)
+            total += some
+            size += (turned_size(f64(g[part]), pairs, layout) * np.abs(norms)).sum((0, 1))
+        # a term is off by 32 units; a lane adds up `steps` of each of its wavefront's stretches, six additions join a wavefront's lanes and four a workgroup's
+        # wavefronts, in float32; rows of workgroups are added in float64 and rounded once
+        terms = steps * -(-stretches // waves) + 6 + 4 + 32
+        within(f64(gw), total, (terms * EPS + ANGLE) * size + ROUND[gw.dtype] * np.abs(total), "gradient of the weight")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("heads,dim,page", [(8, 32, 64), (16, 16, 16), (8, 80, 128)])
+def test_append_in_8_bits_of_more_blocks_than_wavefronts(dtype, heads, dim, page):
+    """A wavefront takes two heads of a block, where there are so many blocks."""
+    rng = np.random.default_rng([heads, dim, 74])
+    held, new = [0, 17, 5, 0, 48], [3001, 16, 5000, 0, 1300]
+    assert 2 * (sum(new) // 16 + 2 * len(new)) >= 4 * units()
+    c = make_bytes(rng, held, heads, dim, page, capacity=5120)
+    ends = np.concatenate([[0], np.cumsum(new)])
+    n = int(ends[-1])
+    kv = dev(rng.standard_normal((n, 2 * heads, dim)) * np.exp(2 * rng.standard_normal((n, 2 * heads, 1))), dtype)
+    k, v = kv[:, :heads], kv[:, heads:]
+    want = bytes_append64(c, f64(k), f64(v), held, ends)
+    c.append(k, v, offsets=dev(ends.astype(np.int32)))
+    for x in "kv":
+        same_codes(getattr(c, x + "_pages"), want[x + "_pages"], x)
+        assert np.array_equal(f64(getattr(c, x + "_scale")), want[x + "_scale"], equal_nan=True), x
+    assert c.lengths.tolist() == [a + b for a, b in zip(held, new)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_append_in_8_bits_at_once_and_by_blocks(dtype):
+    """With rotation: one call of many blocks leaves what many calls of few leave."""
+    rng = np.random.default_rng(75)
+    heads, dim, n, step = 8, 64, 9008, 16 * 113
+    rot = cb.Rotary(dim, (8, 12, 12))
+    k, v = (dev(rng.standard_normal((n, heads, dim)) * np.exp(rng.standard_normal((n, 1, 1))), dtype) for _ in range(2))
+    q, pos = dev(rng.standard_normal((n, heads, dim)), dtype), dev(rng.integers(0, 500, (n, 3)).astype(np.int32))
+    a, b = (cb.TokenCache.create(1, heads, dim, n, dtype=E4M3) for _ in range(2))
+    turned = a.append(k, v, pos, rot, q, offsets=dev(np.array([0, n], np.int32)))
+    for i in range(0, n, step):
+        j = min(i + step, n)
+        assert torch.equal(b.append(k[i:j], v[i:j], pos[i:j], rot, q[i:j], offsets=dev(np.array([0, j - i], np.int32))), turned[i:j])
+    for x in ("k_pages", "v_pages"):
+        assert torch.equal(getattr(a, x).view(torch.uint8), getattr(b, x).view(torch.uint8))
+    assert torch.equal(a.k_scale, b.k_scale) and torch.equal(a.v_scale, b.v_scale) and a.lengths.tolist() == b.lengths.tolist() == [n]
