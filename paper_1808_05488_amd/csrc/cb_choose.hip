@@ -6,9 +6,10 @@
 // sums over rows in LDS 21.)
 //
 // Scores.  sum_d max(q_d lo_d, q_d hi_d) is no less than q.k for any key k of the page; a page's score is the largest of its key head's query heads.  Sums
-// are in float64 and rounded to float32 once, so that what is chosen does not depend on their order (products of float32 values are exact there):
+// are in float64 and rounded to float32 once: products of float32 values are exact there, and a sum is off by dim * 2^-53 of its terms' sizes at most, so that their
+// order shows only in scores that lie as near to where float32's rounding changes, or whose terms all but cancel.  The order is fixed, whatever pages and heads a call has:
 // the matrix cores' 4 x 4 x 4 products in four blocks, 16 pages and 4 query heads at once, of hi with the positive parts of q and of lo with the negative
-// ones (vector instructions took 7 us where these take 3: they convert every value for every query head).  Memory bounds it: 2 * dim values a page and key head.
+// ones, each summed by itself (vector instructions took 7 us where these take 3: they convert every value for every query head).  Memory bounds it: 2 * dim values a page and key head.
 //
 // Choice.  The workgroup that comes last of those that have made a (sequence, key head)'s scores finds the lowest score that is taken by counting digits
 // (radix selection, ten bits a pass between the lowest and the highest score), then lists the pages in order.  Sequences whose pages are all taken
@@ -180,7 +181,6 @@ struct ChooseArgs {
 
 __device__ __forceinline__ void put_rank(uint32_t* at, uint32_t r) { __hip_atomic_store(at, r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 // Four of them, as other compute units have written them.
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ u32x4 get_ranks(__amdgpu_buffer_rsrc_t ranks, int at)
 {
     constexpr int AGENT = 16;

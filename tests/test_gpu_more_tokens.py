@@ -1454,3 +1454,32 @@ def test_append_in_8_bits_at_once_and_by_blocks(dtype):
     for x in ("k_pages", "v_pages"):
         assert torch.equal(getattr(a, x).view(torch.uint8), getattr(b, x).view(torch.uint8))
     assert torch.equal(a.k_scale, b.k_scale) and torch.equal(a.v_scale, b.v_scale) and a.lengths.tolist() == b.lengths.tolist() == [n]
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_choose_of_scores_whose_terms_cancel(seed):
+    """Terms of 2^-40 .. 2^40 and of both signs: a score is the exact one but for a rounding a term in float64 and one to float32, and where that leaves two pages
+    in either order either may be chosen."""
+    rng = np.random.default_rng([seed, 76])
+    pages, dim, group, budget = 300, 32, 3, 40
+    k = torch.zeros((pages, 1, 16, dim), device="cuda")
+    lo = rng.standard_normal((pages, dim)) * 2.0 ** rng.integers(-20, 21, (pages, dim))
+    lo[:, 1::2] = -lo[:, ::2] * (1 + 2.0 ** -20 * rng.integers(-1, 2, (pages, dim // 2)))       # (pairs of terms that all but cancel, or do)
+    bounds = dev(np.stack([lo, lo], 1)[:, None].astype(np.float32))
+    q = rng.standard_normal((1, group, dim)) * 2.0 ** rng.integers(-20, 21, (1, group, 1))
+    q[..., 1::2] = q[..., ::2]
+    q = dev(q, F32)
+    c = cb.TokenCache(k, k, torch.arange(pages, dtype=torch.int32, device="cuda")[None], torch.tensor([16 * pages], dtype=torch.int32, device="cuda"), bounds=bounds)
+    chosen, count = c.choose(q, budget)
+    got = chosen[0, 0].tolist()
+    assert count.item() == budget and got == sorted(set(got)) and 0 <= got[0] and got[-1] < pages
+    x, q64 = f64(bounds)[:, 0, 0], f64(q)[0]
+    least, most = np.empty(pages, np.float32), np.empty(pages, np.float32)
+    for p in range(pages):
+        exact = [math.fsum(x[p] * q64[g]) for g in range(group)]                          # (products are exact in float64)
+        off = [(dim + 1) * 2.0 ** -53 * np.abs(x[p] * q64[g]).sum() for g in range(group)]
+        least[p], most[p] = max(a - b for a, b in zip(exact, off)), max(a + b for a, b in zip(exact, off))
+    out = np.setdiff1d(np.arange(pages), got)
+    assert (most[got][:, None] >= least[out][None]).all()
+    sure = [p for p in got if (least[p] > most[out]).all()]
+    assert len(sure) >= budget // 2                                                        # (most of them are no near thing)
