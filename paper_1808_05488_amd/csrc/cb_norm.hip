@@ -76,7 +76,8 @@ template <int VE, bool ADJACENT> __device__ __forceinline__ void turn_by(const f
     }
 }
 
-// PPL: pieces of a head that a lane has (more than one where single values are taken of heads above 128).  CACHED: loads and stores go through the caches.
+// PPL: pieces of a head that a lane has (more than one where single values are taken of heads above 128).  CACHED: loads and stores go through the caches (where they
+// do not, all of a head is turned).
 template <typename T, int VE, int PPL, bool ADJACENT, bool CACHED, bool BACK>
 __global__ __launch_bounds__(THREADS, VE == 8 ? (BACK ? 3 : 4) : 1) void norm_kernel(const NormJob n, const Shape sh)
 {
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(THREADS, VE == 8 ? (BACK ? 3 : 4) : 1) void norm_ke
                 }
                 if constexpr (BACK) {
                     angles(p, at[p]);
-                    turn_by<VE, ADJACENT>(at[p], turns[p], d[p][0], d[p][1]);
+                    turn_by<VE, ADJACENT>(at[p], !CACHED || turns[p], d[p][0], d[p][1]);
                 }
             }
             float mean, dot;
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(THREADS, VE == 8 ? (BACK ? 3 : 4) : 1) void norm_ke
                             if (down != 0) f[p][i][e] = __builtin_ldexpf(f[p][i][e], -down);
                         }
                     }
-                if constexpr (!BACK) turn_by<VE, ADJACENT>(at[p], turns[p], f[p][0], f[p][1]);
+                if constexpr (!BACK) turn_by<VE, ADJACENT>(at[p], !CACHED || turns[p], f[p][0], f[p][1]);
                 if (!there || !stored) continue;
                 V y, z;
 #pragma unroll
