@@ -462,7 +462,10 @@ int cb_norm_rotate_back(const cb_rotary *rotary, int32_t dtype, int64_t n_tokens
  * and scales (positive, finite) themselves.  Eviction refuses such a cache.
  *
  * Bounds (cb_cache_bound, cb_cache_choose) are, for every page and key head, head_dim smallest and head_dim largest values of its tokens'
- * keys, of the cache's type, with CB_E4M3 bfloat16. */
+ * keys, of the cache's type, with CB_E4M3 bfloat16.
+ *
+ * (What stands behind scratch_bytes came with version 0.2.0.  The structure has no size of its own: a caller that was compiled with an
+ * earlier header hands over less than is read, and has to be compiled anew; cb_version() tells.) */
 typedef struct {
     int32_t n_seq, n_kv_heads;        /* n_seq 1 .. 65535, n_kv_heads 1 .. 1024 */
     int32_t head_dim;                 /* a multiple of 8 up to 256 */
